@@ -234,6 +234,19 @@ int specvla_verify_tree(specvla_ctx *ctx, int n_ep, const int *episodes,
                         const specvla_tree *trees, int r, int *accept_len_out, int *tokens_out,
                         float *logits_out, void *stream);
 
+/* Verification by random numbers: as specvla_verify_tree, but a drafted token is accepted against the
+ * target's probabilities (softmax of the logits / temperature, over the ids that the greedy choice ranges
+ * over) instead of its greedy token, and the token after the accepted path is drawn. The rule is that of
+ * specvla_verify_sampled without draft probabilities (the draft tree holds the draft model's best tokens, it
+ * is not drawn from it): whatever the tree, the emitted tokens have the target's distribution. Relaxed
+ * acceptance does not apply.
+ *   temperature  > 0
+ *   u            device f32 [total rows], rows in call order: numbers in [0, 1); the root's draws the last token
+ *   logits       device f32 [total rows, vocab], written and read */
+int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees,
+                                float temperature, const float *u, int *accept_len_out, int *tokens_out,
+                                float *logits, void *stream);
+
 /* The verification forward alone (Eq. 1 over every tree row): greedy token of M_V after each row
  * of caller-supplied trees, WITHOUT acceptance, compaction or any change of the episodes' state
  * (the tree rows' K/V land in cache slots beyond the committed ones and are overwritten by the next
@@ -330,6 +343,110 @@ int specvla_gemm_static(const float *X, const void *W, float *Y, int T, int N, i
                         void *stream);
 /* specvla_gemm_status for the built-in scratch of the current device: synchronises `stream`. */
 int specvla_gemm_static_status(void *stream);
+
+/* ---- Stand-alone operators around a verification step -------------------------------------------------
+ * For programs that run other layers than the decoder's own (an encoder or projector that makes the prefix
+ * embeddings, a quantised head, a target model of their own): RMSNorm to 8 bits, a linear layer with its
+ * epilogue, and the verification of drafted tokens by random numbers. They follow one another as they
+ * stand: codes and scales of the norm are the linear layer's rows, its fp32 output the verification's logits.
+ *  - All pointers are device memory of the current device. Leading dimensions (ld*) are in elements,
+ *    from the start of a row to the start of the next.
+ *  - Calls are asynchronous, allocate nothing and may be captured into a graph. They share no state: calls
+ *    on different streams may overlap as long as their outputs, status words and scratch differ.
+ *  - Outputs must not overlap inputs, except where a call says so.
+ * Element types: */
+#define SPECVLA_F32  0
+#define SPECVLA_BF16 1
+#define SPECVLA_F16  2
+#define SPECVLA_I8   3
+#define SPECVLA_E4M3 4    /* 8-bit float: 4 exponent bits, 3 mantissa bits, largest value 448 */
+
+/* Residual add, RMSNorm and rounding to 8 bits with one scale per row. With C = 127 (SPECVLA_I8) or 448 (E4M3):
+ *   s = x + residual, rounded to `type` (what `sum` receives)          t = s * gain
+ *   codes = round-half-even(t * C / max|t|)        scale = max|t| / C / sqrt(mean(s^2) + eps)
+ * so that codes * scale is the normalised row. The codes are those of exact arithmetic rounded once (decided in 64
+ * bits where 32 could differ). A row of zeros has codes 0 and scale 1. A row with an infinity or a NaN (in s or in
+ * the gain) has codes 0 and scale NaN; no other row is touched by it.
+ * Rows may start anywhere; fastest when every row of x, residual and sum starts on 16 bytes, d is a multiple
+ * of 16 bytes of x and the codes' rows start on 8. */
+typedef struct {
+  int rows, d;
+  int type;                       /* of x, residual and sum: SPECVLA_F32, BF16 or F16 */
+  int code_type;                  /* SPECVLA_I8 or SPECVLA_E4M3 */
+  const void *x;        long long ldx;
+  const void *residual; long long ld_residual;   /* may be NULL */
+  const float *gain;              /* [d], may be NULL: ones */
+  void *sum;            long long ld_sum;        /* may be NULL; may be x or residual itself (same ld) */
+  void *codes;          long long ld_codes;
+  float *scale;                   /* [rows] */
+  float eps;                      /* >= 0 */
+} specvla_norm_args;
+int specvla_rmsnorm_q8(const specvla_norm_args *args, void *stream);
+/* The rounding alone: codes = round-half-even(x * C / max|x|), scale = max|x| / C per row. For weights, or rows that
+ * no norm precedes. */
+int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ldx, void *codes, int code_type,
+                          long long ld_codes, float *scale, void *stream);
+
+/* Y = act(X_scale[t] W_scale[n] (X W^T)[t][n] + bias[n]) + residual[t][n]
+ * X [T, K] and W [N, K] of one type: BF16, F16, I8 or E4M3; scales only for the last two. Products are exact
+ * in the accumulator (int8: 32-bit integers, K <= 131071; otherwise fp32); scales, bias, activation and residual are
+ * applied in fp32 and the result is rounded once to out_type (F32, BF16, F16). Any T, N, K >= 1; rows of X and W
+ * start on 16 bytes (base address and ld); Y and residual on their own element. Y may be the residual itself. Values
+ * that are not finite reach what depends on them only.
+ * status: one word, zeroed by the caller before its first use and left alone by calls that succeed: a bounded
+ * device-side wait that gave up sets it, and specvla_gemm_status(status, stream) then reports
+ * SPECVLA_ERR_TIMEOUT (Y is undefined; zero the word to use it again). */
+#define SPECVLA_ACT_NONE      0
+#define SPECVLA_ACT_RELU      1
+#define SPECVLA_ACT_GELU      2   /* v / 2 (1 + erf(v / sqrt 2)) */
+#define SPECVLA_ACT_GELU_TANH 3   /* v / 2 (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) */
+#define SPECVLA_ACT_SILU      4   /* v / (1 + exp(-v)) */
+typedef struct {
+  int T, N, K;
+  int type, out_type, act;
+  const void *X; long long ldx; const float *x_scale;   /* [T] or NULL: ones */
+  const void *W; long long ldw; const float *w_scale;   /* [N] or NULL: ones */
+  const float *bias;                                    /* [N] or NULL */
+  const void *residual; long long ld_residual;          /* out_type, or NULL */
+  void *Y; long long ldy;
+  int *status;
+} specvla_linear_args;
+int specvla_linear(const specvla_linear_args *args, void *stream);
+/* specvla_gemm_fault_test for the next specvla_linear call of the process. */
+int specvla_linear_fault_test(long long wait_limit_ns, int withhold_k_block);
+
+/* Verification of drafted tokens against the target's probabilities, by given random numbers (speculative
+ * sampling over trees). Row i of tree b is row b * rows + i of logits and draft_probs.
+ *   p_i = softmax(logits_i / temperature) over the ids [lo, hi); a NaN logit counts as -infinity, infinite logits
+ *   share the row, and a row without a number gives its lowest id probability 1.
+ * The walk starts at row 0. Where it stands at row a, a's children c are tried in ascending order, x = tokens[c]:
+ *   with draft_probs (q_a = the distribution from which the children of a were drawn, independently; values
+ *   that are not positive count as 0): beta = 0, S = 1; accepted when u_c q_a(x) S < max(p_a(x) - beta q_a(x), 0), else
+ *   beta += S and S = sum_x max(p_a(x) - beta q_a(x), 0);
+ *   without: accepted when u_c S < p_a(x), S = the sum of p_a without the tokens refused at a so far; a token that was
+ *   refused at a has p_a = 0 from then on.
+ * At an accepted child the walk goes on. Where none is accepted (or there is none), the next token is drawn from what is
+ * left (max(p - beta q, 0), or p without the refused tokens; p itself if nothing is): the first id whose
+ * cumulative weight exceeds u_0 times the total. All of it is 64-bit arithmetic.
+ * A child whose token is outside [lo, hi) is never accepted; a row whose parent is not a row before it belongs to
+ * no tree. n_rows outside 1 .. rows is taken as the nearest of the two. */
+typedef struct {
+  int n_seq, rows;                /* trees; rows of each in the arrays, <= SPECVLA_MAX_TREE_ROWS */
+  int vocab, lo, hi;              /* at most 2^20 ids may take part */
+  int logits_type;                /* SPECVLA_F32, BF16 or F16 */
+  const void *logits; long long ld_logits;
+  const float *draft_probs; long long ld_draft;         /* [n_seq * rows][vocab] or NULL */
+  float temperature;              /* > 0 */
+  const int *tokens, *parent;     /* [n_seq][rows]; row 0 is the root */
+  const int *n_rows;              /* [n_seq] or NULL: all rows */
+  const float *u;                 /* [n_seq][rows] in [0, 1): u of row i >= 1 decides it, u of row 0 draws the last token */
+  int *accept_len;                /* [n_seq]: accepted tokens m */
+  int *path;                      /* [n_seq][rows]: 0 and the m accepted rows, then -1 */
+  int *tokens_out;                /* [n_seq][rows]: their m tokens and the one after them, then -1 */
+} specvla_verify_args;
+/* scratch: device, 8-byte aligned, one per call in flight; 0 is returned for sizes out of range. */
+size_t specvla_verify_sampled_scratch_bytes(int n_seq, int rows, int lo, int hi);
+int specvla_verify_sampled(const specvla_verify_args *args, void *scratch, size_t scratch_bytes, void *stream);
 
 /* Per-GEMM device timing (measurement aid; Section 3.1 attributes the latency to the
  * parameter stream, which these GEMMs are). `phases` is a bit mask: 1 = prefill, 2 = draft,

@@ -53,6 +53,28 @@ class Stats(C.Structure):
                 ("ms_loop", C.c_float), ("device_loop", C.c_int)]
 
 
+class NormArgs(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rows", "d", "type", "code_type")] + \
+               [("x", C.c_void_p), ("ldx", C.c_longlong), ("residual", C.c_void_p), ("ld_residual", C.c_longlong),
+                ("gain", C.c_void_p), ("sum", C.c_void_p), ("ld_sum", C.c_longlong),
+                ("codes", C.c_void_p), ("ld_codes", C.c_longlong), ("scale", C.c_void_p), ("eps", C.c_float)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("T", "N", "K", "type", "out_type", "act")] + \
+               [("X", C.c_void_p), ("ldx", C.c_longlong), ("x_scale", C.c_void_p),
+                ("W", C.c_void_p), ("ldw", C.c_longlong), ("w_scale", C.c_void_p), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ld_residual", C.c_longlong), ("Y", C.c_void_p), ("ldy", C.c_longlong),
+                ("status", C.c_void_p)]
+
+
+class VerifyArgs(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_seq", "rows", "vocab", "lo", "hi", "logits_type")] + \
+               [("logits", C.c_void_p), ("ld_logits", C.c_longlong), ("draft_probs", C.c_void_p),
+                ("ld_draft", C.c_longlong), ("temperature", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("tokens", "parent", "n_rows", "u", "accept_len", "path", "tokens_out")]
+
+
 EXPORTS = {
     "specvla_workspace_bytes": (C.c_size_t, [C.POINTER(ModelDesc)]),
     "specvla_create": (C.c_int, [C.POINTER(ModelDesc), C.POINTER(Weights), C.POINTER(DraftWeights),
@@ -87,6 +109,16 @@ EXPORTS = {
     "specvla_gemm_static_status": (C.c_int, [C.c_void_p]),
     "specvla_gemm_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int,
                                      C.c_void_p]),
+    "specvla_verify_tree_sampled": (C.c_int, [C.c_void_p, C.c_int, C.POINTER(C.c_int), C.POINTER(Tree), C.c_float,
+                                              C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int), C.c_void_p,
+                                              C.c_void_p]),
+    "specvla_rmsnorm_q8": (C.c_int, [C.POINTER(NormArgs), C.c_void_p]),
+    "specvla_quantize_rows": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_longlong, C.c_void_p, C.c_int,
+                                        C.c_longlong, C.c_void_p, C.c_void_p]),
+    "specvla_linear": (C.c_int, [C.POINTER(LinearArgs), C.c_void_p]),
+    "specvla_linear_fault_test": (C.c_int, [C.c_longlong, C.c_int]),
+    "specvla_verify_sampled_scratch_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int]),
+    "specvla_verify_sampled": (C.c_int, [C.POINTER(VerifyArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
     "specvla_profile": (C.c_int, [C.c_void_p, C.c_int]),
     "specvla_profile_read": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_longlong),
                                        C.POINTER(C.c_double)]),
@@ -246,6 +278,35 @@ class SpecVLA:
         emitted = [list(toks[i * (MAX_DEPTH + 1): i * (MAX_DEPTH + 1) + m[i] + 1]) for i in range(n)]
         return (list(m), emitted, logits) if want_logits else (list(m), emitted)
 
+    def verify_tree_sampled(self, episodes, trees, u, temperature=1.0):
+        """verify_tree with acceptance by random numbers: u is a CUDA f32 tensor of one number per row, rows in
+        call order. trees as in verify_tree; for the device-resident ones (None) u has as many rows as they have.
+        Returns (accept lengths, emitted tokens per episode, logits [rows, V])."""
+        n = len(episodes)
+        ctrees, keep, rows = None, [], 0
+        if trees is not None:
+            ctrees = (Tree * n)()
+            for i, t in enumerate(trees):
+                a, b, c = _ints(t["tokens"]), _ints(t["parent"]), _ints(t["depth"])
+                keep += [a, b, c]
+                ctrees[i].n_rows = len(t["tokens"])
+                ctrees[i].tokens, ctrees[i].parent, ctrees[i].depth = a, b, c
+                ctrees[i].score = None
+                rows += len(t["tokens"])
+            if rows != u.numel():
+                raise ValueError(f"{u.numel()} random numbers for {rows} rows")
+        _check_cuda(u)
+        if u.dtype != torch.float32 or not u.is_contiguous():
+            raise ValueError("u must be a contiguous float32 tensor")
+        logits = torch.empty(u.numel(), self.model.vocab, dtype=torch.float32, device="cuda")
+        m = (C.c_int * n)()
+        toks = (C.c_int * (n * (MAX_DEPTH + 1)))()
+        self._check(lib.specvla_verify_tree_sampled(self.h, n, _ints(episodes), ctrees, float(temperature),
+                                                    C.c_void_p(u.data_ptr()), m, toks, C.c_void_p(logits.data_ptr()),
+                                                    _stream()))
+        emitted = [list(toks[i * (MAX_DEPTH + 1): i * (MAX_DEPTH + 1) + m[i] + 1]) for i in range(n)]
+        return list(m), emitted, logits
+
     def score_tree(self, episodes, trees):
         """Greedy token of the target after every row of the given trees; episode state untouched."""
         n = len(episodes)
@@ -385,3 +446,185 @@ class GemmRunner:
         if rc != 0:
             raise SpecVLAError(rc)
         return self.y
+
+
+# ---------------------------------------------------------------------- stand-alone operators
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, torch.float8_e4m3fn: 4}
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
+_CODES = (torch.int8, torch.float8_e4m3fn)
+_status_words = {}
+
+
+def _check_cuda(*tensors):
+    """The library works on the current device: tensors elsewhere are refused."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"tensor on {t.device}, current device is cuda:{dev}")
+
+
+def _rows(t, name, shape=None, dtypes=None):
+    """A matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise ValueError(f"{name} has type {t.dtype}")
+    return t
+
+
+def _vector(t, name, n):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous float32 vector of {n}")
+    return t
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _ld(t):
+    return 0 if t is None else max(t.stride(0), t.shape[1])
+
+
+def _run(rc):
+    if rc != 0:
+        raise SpecVLAError(rc)
+
+
+def rmsnorm_q8(x, gain=None, residual=None, eps=1e-6, dtype=torch.int8, out_sum=None):
+    """specvla_rmsnorm_q8 over the rows of x [rows, d] (f32 / bf16 / f16): codes (int8 or float8_e4m3fn), scale
+    [rows], and the sum x + residual in x's type (None without a residual). out_sum: where the sum goes; x and
+    residual themselves are allowed."""
+    _rows(x, "x", dtypes=_FLOATS)
+    rows, d = x.shape
+    if dtype not in _CODES:
+        raise ValueError(f"codes of type {dtype}")
+    _vector(gain, "gain", d)
+    total = None
+    if residual is not None:
+        _rows(residual, "residual", x.shape, (x.dtype,))
+        total = torch.empty_like(x, memory_format=torch.contiguous_format) if out_sum is None else \
+            _rows(out_sum, "out_sum", x.shape, (x.dtype,))
+    elif out_sum is not None:
+        raise ValueError("out_sum without a residual")
+    _check_cuda(x, gain, residual, total)
+    codes = torch.empty(rows, d, dtype=dtype, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rows and d:
+        _run(lib.specvla_rmsnorm_q8(C.byref(NormArgs(
+            rows, d, TYPES[x.dtype], TYPES[dtype], x.data_ptr(), _ld(x), _ptr(residual), _ld(residual), _ptr(gain),
+            _ptr(total), _ld(total), codes.data_ptr(), d, scale.data_ptr(), eps)), _stream()))
+    return codes, scale, total
+
+
+def quantize_rows(x, dtype=torch.int8):
+    """specvla_quantize_rows over the rows of x [rows, d]: codes and scale [rows]."""
+    _rows(x, "x", dtypes=_FLOATS)
+    if dtype not in _CODES:
+        raise ValueError(f"codes of type {dtype}")
+    _check_cuda(x)
+    rows, d = x.shape
+    codes = torch.empty(rows, d, dtype=dtype, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rows and d:
+        _run(lib.specvla_quantize_rows(C.c_void_p(x.data_ptr()), TYPES[x.dtype], rows, d, _ld(x),
+                                       C.c_void_p(codes.data_ptr()), TYPES[dtype], d, C.c_void_p(scale.data_ptr()),
+                                       _stream()))
+    return codes, scale
+
+
+def _status_word():
+    """The status word of this module's linear() calls on the current device (linear_status reads it)."""
+    dev = torch.cuda.current_device()
+    if dev not in _status_words:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first linear() on a device must not be inside a stream capture")
+        _status_words[dev] = torch.zeros(1, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+    return _status_words[dev]
+
+
+def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=None, dtype=None, out=None):
+    """specvla_linear: act(x @ w.T * scales + bias) + residual. x [T, K] and w [N, K] of one type (bf16, f16, int8,
+    float8_e4m3fn), scales f32 [T] and [N] with the 8-bit ones, bias f32 [N]; dtype: of the result and the residual
+    (default: x's, bf16 for 8-bit operands). out: where the result goes, the residual itself is allowed.
+    Asynchronous: linear_status() reports a device-side wait that gave up."""
+    _rows(x, "x", dtypes=(torch.bfloat16, torch.float16) + _CODES)
+    T, K = x.shape
+    _rows(w, "w", (w.shape[0], K), (x.dtype,))
+    N = w.shape[0]
+    if dtype is None:
+        dtype = out.dtype if out is not None else torch.bfloat16 if x.dtype in _CODES else x.dtype
+    if dtype not in _FLOATS:
+        raise ValueError(f"result of type {dtype}")
+    if act not in ACTS:
+        raise ValueError(f"activation {act!r}: one of {', '.join(ACTS)}")
+    if (x_scale is not None or w_scale is not None) and x.dtype not in _CODES:
+        raise ValueError("scales belong to 8-bit operands")
+    _vector(bias, "bias", N), _vector(x_scale, "x_scale", T), _vector(w_scale, "w_scale", N)
+    if residual is not None:
+        _rows(residual, "residual", (T, N), (dtype,))
+    y = torch.empty(T, N, dtype=dtype, device=x.device) if out is None else _rows(out, "out", (T, N), (dtype,))
+    _check_cuda(x, w, bias, residual, x_scale, w_scale, y)
+    if T and N:
+        if not K:
+            raise ValueError("K is 0")
+        _run(lib.specvla_linear(C.byref(LinearArgs(
+            T, N, K, TYPES[x.dtype], TYPES[dtype], ACTS[act], x.data_ptr(), _ld(x), _ptr(x_scale), w.data_ptr(), _ld(w),
+            _ptr(w_scale), _ptr(bias), _ptr(residual), _ld(residual), y.data_ptr(), _ld(y),
+            _status_word().data_ptr())), _stream()))
+    return y
+
+
+def linear_status():
+    """Synchronises the current stream; raises SpecVLAError(-6) if a linear() call on this device gave up since the
+    last time (its result is undefined), and clears the status."""
+    word = _status_word()
+    rc = lib.specvla_gemm_status(C.c_void_p(word.data_ptr()), _stream())
+    if rc != 0:
+        word.zero_()
+    _run(rc)
+
+
+def verify_sampled(logits, tokens, parent, u, n_rows=None, temperature=1.0, draft_probs=None, lo=0, hi=None):
+    """specvla_verify_sampled: logits [trees, rows, V] (f32 / bf16 / f16), tokens and parent [trees, rows] int32, u
+    [trees, rows] f32, n_rows [trees] int32 or None, draft_probs [trees, rows, V] f32 or None; ids [lo, hi) take part.
+    Returns accept lengths [trees], path and tokens [trees, rows] (int32, -1 behind their ends)."""
+    if logits.dim() != 3 or logits.dtype not in _FLOATS:
+        raise ValueError("logits must be [trees, rows, vocab] of f32, bf16 or f16")
+    n, rows, vocab = logits.shape
+    hi = vocab if hi is None else hi
+
+    def flat(t, name):
+        if tuple(t.shape) != (n, rows, vocab) or t.stride(2) != 1 or (n > 1 and t.stride(0) != rows * t.stride(1)) or \
+                (n * rows > 1 and t.stride(1) < vocab):
+            raise ValueError(f"{name} must be [{n}, {rows}, {vocab}] with rows at one distance")
+        return max(t.stride(1), vocab)
+
+    ld = flat(logits, "logits")
+    ldp = 0
+    if draft_probs is not None:
+        if draft_probs.dtype != torch.float32:
+            raise ValueError("draft_probs must be float32")
+        ldp = flat(draft_probs, "draft_probs")
+    for t, name, dt, shape in ((tokens, "tokens", torch.int32, (n, rows)), (parent, "parent", torch.int32, (n, rows)),
+                               (u, "u", torch.float32, (n, rows)), (n_rows, "n_rows", torch.int32, (n,))):
+        if t is not None and (t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {dt} {shape}")
+    _check_cuda(logits, tokens, parent, u, n_rows, draft_probs)
+    m = torch.empty(n, dtype=torch.int32, device=logits.device)
+    path = torch.empty(n, rows, dtype=torch.int32, device=logits.device)
+    out = torch.empty(n, rows, dtype=torch.int32, device=logits.device)
+    if n:
+        nb = lib.specvla_verify_sampled_scratch_bytes(n, rows, lo, hi)
+        if nb == 0:
+            raise SpecVLAError(-1, f"({n} trees of {rows} rows over ids [{lo}, {hi}))")
+        scratch = torch.empty(nb, dtype=torch.uint8, device=logits.device)
+        _run(lib.specvla_verify_sampled(C.byref(VerifyArgs(
+            n, rows, vocab, lo, hi, TYPES[logits.dtype], logits.data_ptr(), ld, _ptr(draft_probs), ldp, temperature,
+            tokens.data_ptr(), parent.data_ptr(), _ptr(n_rows), u.data_ptr(), m.data_ptr(), path.data_ptr(),
+            out.data_ptr())), C.c_void_p(scratch.data_ptr()), nb, _stream()))
+    return m, path, out

@@ -1,0 +1,255 @@
+// Entry points of the stand-alone operators (see include/specvla.h): RMSNorm to 8 bits, the linear layer with its
+// epilogue, verification of drafted tokens by random numbers.
+#include "../../include/specvla.h"
+
+#include <string.h>
+
+#include <algorithm>
+#include <climits>
+#include <mutex>
+
+#include "linear.cuh"
+#include "norm_q8.cuh"
+#include "sampled.cuh"
+
+namespace {
+
+size_t bytes_of(int type) {
+  switch (type) {
+    case SPECVLA_F32: return 4;
+    case SPECVLA_BF16: case SPECVLA_F16: return 2;
+    case SPECVLA_I8: case SPECVLA_E4M3: return 1;
+    default: return 0;
+  }
+}
+bool is_float(int type) { return type == SPECVLA_F32 || type == SPECVLA_BF16 || type == SPECVLA_F16; }
+bool is_code(int type) { return type == SPECVLA_I8 || type == SPECVLA_E4M3; }
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// Every kernel here may start beside its predecessor and waits for it before it touches memory. A launch that is
+// refused fails this call and no other.
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, int cluster, void *stream, A... args) {
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess) return SPECVLA_OK;
+  cudaGetLastError();
+  return SPECVLA_ERR_CUDA;
+}
+
+// ------------------------------------------------------------------ RMSNorm to 8 bits
+template <typename T, int CODE>
+int norm_launch(const norm_q8::Args &a, int rows, void *stream) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool vec = a.d % V == 0 && aligned(a.x, 16) && a.ldx % V == 0 && (!a.r || (aligned(a.r, 16) && a.ldr % V == 0)) &&
+                   (!a.s || (aligned(a.s, 16) && a.lds % V == 0)) && (!a.gain || aligned(a.gain, 16)) &&
+                   aligned(a.q, V) && a.ldq % V == 0;
+  // as many vectors a thread as it keeps; with fewer rows than SMs one, so that all loads are in flight at once
+  const long long n = (a.d + (vec ? V : 1) - 1) / (vec ? V : 1);
+  const long long per = rows <= 148 ? 1 : norm_q8::cached(vec ? V : 1);
+  const int threads = (int)std::min(1024ll, std::max(64ll, (n + 32 * per - 1) / (32 * per) * 32));
+  return launch(vec ? norm_q8::norm_q8_kernel<T, CODE, V> : norm_q8::norm_q8_kernel<T, CODE, 1>, dim3(rows), dim3(threads), 0, 1,
+                stream, a);
+}
+int norm_entry(const norm_q8::Args &a, int rows, int type, int code_type, void *stream) {
+  const bool i8 = code_type == SPECVLA_I8;
+  using namespace norm_q8;
+  switch (type) {
+    case SPECVLA_F32: return i8 ? norm_launch<float, CODE_I8>(a, rows, stream) : norm_launch<float, CODE_E4M3>(a, rows, stream);
+    case SPECVLA_BF16: return i8 ? norm_launch<bf16, CODE_I8>(a, rows, stream) : norm_launch<bf16, CODE_E4M3>(a, rows, stream);
+    default: return i8 ? norm_launch<__half, CODE_I8>(a, rows, stream) : norm_launch<__half, CODE_E4M3>(a, rows, stream);
+  }
+}
+
+// ------------------------------------------------------------------ linear layer
+constexpr int MAX_DEVICES = 64;
+std::mutex g_mutex;
+struct Fit { bool known; int clusters[linear::MAX_S + 1]; } g_fit[MAX_DEVICES];
+
+// Clusters of S CTAs that are resident at once, per device; 0: unknown.
+const Fit *cluster_fit() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return nullptr;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  Fit &f = g_fit[dev];
+  if (f.known) return &f;
+  auto kernel = linear::linear_slice_kernel<linear::KIND_16, float>;
+  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, linear::SMEM);
+  for (int S = 1; S <= linear::MAX_S; S++) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(S * 64);
+    cfg.blockDim = dim3(linear::THREADS);
+    cfg.dynamicSmemBytes = linear::SMEM;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = S;
+    at.val.clusterDim.y = 1;
+    at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess) f.clusters[S] = n;
+  }
+  cudaGetLastError();
+  f.known = true;
+  return &f;
+}
+
+template <int KIND, typename OUT>
+int linear_launch(const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, int tiles, int chunks, int S, void *stream) {
+  auto kernel = linear::linear_slice_kernel<KIND, OUT>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, linear::SMEM) != cudaSuccess) {
+    cudaGetLastError();
+    return SPECVLA_ERR_CUDA;
+  }
+  return launch(kernel, dim3(tiles * S, chunks), dim3(linear::THREADS), linear::SMEM, S, stream, mw, mx, a, S);
+}
+template <int KIND>
+int linear_out(int out_type, const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, int tiles, int chunks, int S, void *stream) {
+  switch (out_type) {
+    case SPECVLA_F32: return linear_launch<KIND, float>(mw, mx, a, tiles, chunks, S, stream);
+    case SPECVLA_BF16: return linear_launch<KIND, bf16>(mw, mx, a, tiles, chunks, S, stream);
+    default: return linear_launch<KIND, __half>(mw, mx, a, tiles, chunks, S, stream);
+  }
+}
+
+unsigned long long g_linear_wait_ns = gemm_tc::WAIT_LIMIT_NS;    // of the next call (specvla_linear_fault_test)
+int g_linear_withhold = 0;
+
+}  // namespace
+
+int specvla_rmsnorm_q8(const specvla_norm_args *n, void *stream) {
+  if (!n || !n->x || !n->codes || !n->scale || n->rows < 1 || n->d < 1 || !is_float(n->type) || !is_code(n->code_type))
+    return SPECVLA_ERR_INVALID_ARG;
+  if (n->ldx < n->d || n->ld_codes < n->d || (n->residual && n->ld_residual < n->d) || (n->sum && n->ld_sum < n->d) || !(n->eps >= 0.f))
+    return SPECVLA_ERR_INVALID_ARG;
+  const size_t e = bytes_of(n->type);
+  if (!aligned(n->x, e) || !aligned(n->residual, e) || !aligned(n->sum, e) || !aligned(n->gain, 4) || !aligned(n->scale, 4))
+    return SPECVLA_ERR_INVALID_ARG;
+  const norm_q8::Args a = {n->x, n->residual, n->gain, n->sum, static_cast<unsigned char *>(n->codes), n->scale, n->d,
+                           n->ldx, n->ld_residual, n->ld_sum, n->ld_codes, n->eps, 1};
+  return norm_entry(a, n->rows, n->type, n->code_type, stream);
+}
+
+int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ldx, void *codes, int code_type,
+                          long long ld_codes, float *scale, void *stream) {
+  if (!X || !codes || !scale || rows < 1 || d < 1 || ldx < d || ld_codes < d || !is_float(type) || !is_code(code_type) ||
+      !aligned(X, bytes_of(type)) || !aligned(scale, 4))
+    return SPECVLA_ERR_INVALID_ARG;
+  const norm_q8::Args a = {X, nullptr, nullptr, nullptr, static_cast<unsigned char *>(codes), scale, d, ldx, 0, 0, ld_codes, 0.f, 0};
+  return norm_entry(a, rows, type, code_type, stream);
+}
+
+int specvla_linear_fault_test(long long wait_limit_ns, int withhold_k_block) {
+  if (wait_limit_ns < 1000 || withhold_k_block < -1) return SPECVLA_ERR_INVALID_ARG;
+  g_linear_wait_ns = (unsigned long long)wait_limit_ns;
+  g_linear_withhold = withhold_k_block + 1;
+  return SPECVLA_OK;
+}
+
+int specvla_linear(const specvla_linear_args *l, void *stream) {
+  if (!l || !l->X || !l->W || !l->Y || !l->status || l->T < 1 || l->N < 1 || l->K < 1) return SPECVLA_ERR_INVALID_ARG;
+  const bool codes = is_code(l->type);
+  if (!(codes || l->type == SPECVLA_BF16 || l->type == SPECVLA_F16) || !is_float(l->out_type)) return SPECVLA_ERR_INVALID_ARG;
+  if (l->act < SPECVLA_ACT_NONE || l->act > SPECVLA_ACT_SILU) return SPECVLA_ERR_INVALID_ARG;
+  if (!codes && (l->x_scale || l->w_scale)) return SPECVLA_ERR_INVALID_ARG;
+  if (l->type == SPECVLA_I8 && l->K > 131071) return SPECVLA_ERR_INVALID_ARG;       // 2^14 K must fit 31 bits
+  const long long e = (long long)bytes_of(l->type), eo = (long long)bytes_of(l->out_type);
+  // (a single row has no distance to the next)
+  const long long bytes = l->K * e, one = (bytes + 15) / 16 * 16;
+  const long long ldx = l->T == 1 ? one : l->ldx * e, ldw = l->N == 1 ? one : l->ldw * e;
+  if ((l->T > 1 && l->ldx < l->K) || (l->N > 1 && l->ldw < l->K) || ldx % 16 || ldw % 16 || !aligned(l->X, 16) || !aligned(l->W, 16))
+    return SPECVLA_ERR_INVALID_ARG;
+  if ((l->T > 1 && (l->ldy < l->N || (l->residual && l->ld_residual < l->N))) || !aligned(l->Y, eo) || !aligned(l->residual, eo) ||
+      !aligned(l->x_scale, 4) || !aligned(l->w_scale, 4) || !aligned(l->bias, 4) || !aligned(l->status, 4))
+    return SPECVLA_ERR_INVALID_ARG;
+  linear::Args a = {};
+  a.T = l->T, a.N = l->N;
+  a.KB = (int)((bytes + linear::KBYTES - 1) / linear::KBYTES);
+  a.act = l->act;
+  a.pairs = aligned(l->Y, 2 * eo) && (l->T == 1 || l->ldy % 2 == 0) &&
+            (!l->residual || (aligned(l->residual, 2 * eo) && (l->T == 1 || l->ld_residual % 2 == 0)));
+  a.x_scale = l->x_scale, a.w_scale = l->w_scale, a.bias = l->bias;
+  a.res = l->residual, a.ldr = l->ld_residual;
+  a.y = l->Y, a.ldy = l->ldy;
+  a.status = l->status;
+  a.wait_ns = g_linear_wait_ns;
+  a.withhold = g_linear_withhold;
+  g_linear_wait_ns = gemm_tc::WAIT_LIMIT_NS;                     // the test hook holds for one call
+  g_linear_withhold = 0;
+  const int kind = l->type == SPECVLA_I8 ? linear::KIND_I8 : l->type == SPECVLA_E4M3 ? linear::KIND_E4M3 : linear::KIND_16;
+  const int tiles = (l->N + linear::BM - 1) / linear::BM;
+  int chunks = (l->T + linear::MAX_TN - 1) / linear::MAX_TN;
+  a.tn = ((l->T + chunks - 1) / chunks + 15) / 16 * 16;
+  chunks = (l->T + a.tn - 1) / a.tn;
+  if (chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
+  // K slices: as many as run at once, four K blocks each at least
+  int S = 1;
+  const Fit *fit = cluster_fit();
+  for (int s = 2; fit && s <= linear::MAX_S; s++)
+    if ((long long)fit->clusters[s] >= (long long)tiles * chunks && a.KB / s >= 4) S = s;
+  a.idesc = linear::make_idesc(kind, l->type == SPECVLA_BF16, linear::BM, a.tn);
+  CUtensorMap mw, mx;
+  if (!linear::make_map(&mw, l->W, l->N, bytes, ldw, linear::BM) || !linear::make_map(&mx, l->X, l->T, bytes, ldx, a.tn)) {
+    cudaGetLastError();
+    return SPECVLA_ERR_CUDA;
+  }
+  switch (kind) {
+    case linear::KIND_16: return linear_out<linear::KIND_16>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
+    case linear::KIND_I8: return linear_out<linear::KIND_I8>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
+    default: return linear_out<linear::KIND_E4M3>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
+  }
+}
+
+// ------------------------------------------------------------------ verification by random numbers
+size_t specvla_verify_sampled_scratch_bytes(int n_seq, int rows, int lo, int hi) {
+  if (n_seq < 1 || rows < 1 || rows > SPECVLA_MAX_TREE_ROWS || lo < 0 || hi <= lo || hi - lo > sampled::MAX_IDS ||
+      n_seq > INT_MAX / (rows * sampled::CLUSTER))
+    return 0;
+  const size_t pieces = (size_t)n_seq * rows * sampled::pieces_of(hi - lo);
+  return pieces * (sizeof(double) + sizeof(float));
+}
+
+int specvla_verify_sampled(const specvla_verify_args *v, void *scratch, size_t scratch_bytes, void *stream) {
+  if (!v || !v->logits || !v->tokens || !v->parent || !v->u || !v->accept_len || !v->path || !v->tokens_out || !scratch)
+    return SPECVLA_ERR_INVALID_ARG;
+  const size_t need = specvla_verify_sampled_scratch_bytes(v->n_seq, v->rows, v->lo, v->hi);
+  if (need == 0 || v->hi > v->vocab || v->ld_logits < v->vocab || (v->draft_probs && v->ld_draft < v->vocab) || !is_float(v->logits_type) ||
+      !(v->temperature > 0.f) || v->temperature > 3e38f)
+    return SPECVLA_ERR_INVALID_ARG;
+  if (!aligned(scratch, 8) || !aligned(v->logits, bytes_of(v->logits_type)) || !aligned(v->draft_probs, 4) || !aligned(v->tokens, 4) ||
+      !aligned(v->parent, 4) || !aligned(v->n_rows, 4) || !aligned(v->u, 4) || !aligned(v->accept_len, 4) || !aligned(v->path, 4) ||
+      !aligned(v->tokens_out, 4))
+    return SPECVLA_ERR_INVALID_ARG;
+  if (scratch_bytes < need) return SPECVLA_ERR_CAPACITY;
+  sampled::Args a = {};
+  a.logits = v->logits, a.ld = v->ld_logits;
+  a.probs = v->draft_probs, a.ld_probs = v->ld_draft;
+  a.lo = v->lo, a.hi = v->hi;
+  a.n_sub = sampled::pieces_of(v->hi - v->lo);
+  a.temperature = v->temperature;
+  a.u = v->u;
+  a.tokens = v->tokens, a.parent = v->parent, a.n_rows = v->n_rows;
+  a.rows = v->rows;
+  a.sub_sum = static_cast<double *>(scratch);
+  a.sub_max = reinterpret_cast<float *>(a.sub_sum + (size_t)v->n_seq * v->rows * a.n_sub);
+  a.out_m = v->accept_len, a.out_tok = v->tokens_out, a.out_path = v->path;
+  a.out_width = v->rows;
+  const EpArgs none = {};
+  return sampled::enqueue<false>(a, none, v->logits_type == SPECVLA_F32 ? 0 : v->logits_type == SPECVLA_BF16 ? 1 : 2, v->n_seq,
+                                 v->n_seq * v->rows, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? SPECVLA_OK
+             : (cudaGetLastError(), SPECVLA_ERR_CUDA);
+}

@@ -20,6 +20,7 @@
 #include "forward_pk.cuh"
 #include "gemm_ck.cuh"
 #include "gemm_tc.cuh"
+#include "sampled.cuh"
 #include "tree.cuh"
 
 namespace {
@@ -1285,8 +1286,9 @@ static int draft_readback(specvla_ctx *ctx, int n_ep, const int *episodes, specv
 // Verification of the device-resident trees of the episodes in `ea` (rows already counted):
 // forward, greedy tokens, acceptance, path selection, compaction, state update. Results stay
 // on the device (out_m / out_tok / out_path); the caller reads them back.
+// u: acceptance by random numbers at this temperature (needs logits_out); NULL: relaxed acceptance by r.
 static int verify_device_trees(specvla_ctx *ctx, const EpArgs &ea, int R, int r, float *logits_out,
-                               cudaStream_t st) {
+                               cudaStream_t st, const float *u = nullptr, float temperature = 1.f) {
   const specvla_model_desc &d = ctx->desc;
   const int n_ep = ea.n_ep;
   ctx->phase = 4;
@@ -1298,9 +1300,32 @@ static int verify_device_trees(specvla_ctx *ctx, const EpArgs &ea, int R, int r,
     TRY(lm_head_greedy(ctx, ctx->xn, ctx->ssq, R, logits_out, st));
   }
   ctx->feat_valid = false;
-  LAUNCH(tree::accept_select_kernel, dim3(n_ep), dim3(128), ea, ctx->trees, ctx->st, (const int *)ctx->greedy, r,
-         d.action_base, d.n_bins, (const float *)ctx->x, ctx->last_ssq, ctx->last_nt, ctx->final_norm,
-         d.rms_eps, d.d_model, ctx->pend_feat, ctx->out_m, ctx->out_tok, ctx->out_path);
+  if (u) {
+    sampled::Args a = {};
+    a.logits = logits_out;
+    a.ld = d.vocab;
+    argmax_range(ctx, &a.lo, &a.hi);
+    a.n_sub = sampled::pieces_of(a.hi - a.lo);
+    a.temperature = temperature;
+    a.u = u;
+    a.trees = ctx->trees;
+    // (the greedy argmax is done with its candidates: 16 bytes per 128 ids and row, where 12 per 512 are needed)
+    a.sub_sum = reinterpret_cast<double *>(ctx->cand);
+    a.sub_max = reinterpret_cast<float *>(a.sub_sum + (size_t)R * a.n_sub);
+    a.out_m = ctx->out_m;
+    a.out_tok = ctx->out_tok;
+    a.out_path = ctx->out_path;
+    a.out_width = SV_MAX_DEPTH + 1;
+    CU(sampled::enqueue<true>(a, ea, 0, n_ep, R, st));
+    ctx->launches += 2;
+    LAUNCH(tree::commit_path_kernel, dim3(n_ep), dim3(128), ea, ctx->st, (const float *)ctx->x, ctx->last_ssq, ctx->last_nt,
+           ctx->final_norm, d.rms_eps, d.d_model, ctx->pend_feat, (const int *)ctx->out_m, (const int *)ctx->out_tok,
+           (const int *)ctx->out_path);
+  } else {
+    LAUNCH(tree::accept_select_kernel, dim3(n_ep), dim3(128), ea, ctx->trees, ctx->st, (const int *)ctx->greedy, r,
+           d.action_base, d.n_bins, (const float *)ctx->x, ctx->last_ssq, ctx->last_nt, ctx->final_norm,
+           d.rms_eps, d.d_model, ctx->pend_feat, ctx->out_m, ctx->out_tok, ctx->out_path);
+  }
   LAUNCH(tree::kv_compact_kernel, dim3(d.n_layers * 2, n_ep), dim3(256), ea, (const EpState *)ctx->st,
          (const int *)ctx->out_m, (const int *)ctx->out_path, ctx->kv_t, ctx->kv_t_ep_stride,
          ctx->kv_t_layer_stride, d.max_seq, ctx->hd);
@@ -1389,6 +1414,19 @@ int specvla_verify_tree(specvla_ctx *ctx, int n_ep, const int *episodes, const s
   int R = 0;
   TRY(prepare_trees(ctx, n_ep, episodes, trees, &ea, &R, st));
   TRY(verify_device_trees(ctx, ea, R, r, logits_out, st));
+  return finish_verify(ctx, ea, accept_len_out, tokens_out, st);
+}
+
+int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees,
+                                float temperature, const float *u, int *accept_len_out, int *tokens_out,
+                                float *logits, void *stream) {
+  TRY(check_episodes(ctx, n_ep, episodes));
+  if (!(temperature > 0.f) || temperature > 3e38f || !u || !accept_len_out || !tokens_out || !logits) return SPECVLA_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  EpArgs ea{};
+  int R = 0;
+  TRY(prepare_trees(ctx, n_ep, episodes, trees, &ea, &R, st));
+  TRY(verify_device_trees(ctx, ea, R, 0, logits, st, u, temperature));
   return finish_verify(ctx, ea, accept_len_out, tokens_out, st);
 }
 

@@ -383,6 +383,23 @@ rerank_keep_kernel(EpArgs a, DevTree *trees, int keep) {
   if (i == 0) tr.n_rows = 1 + keep;
 }
 
+// Features (final-norm outputs) of the m + 1 rows on an episode's path, for the draft model's next call.
+__device__ __forceinline__ void store_path_features(int e, int base, int m, const int *path, const float *__restrict__ x,
+                                                    const float *__restrict__ ssq, int nt, const float *__restrict__ gain,
+                                                    float eps, int d, float *__restrict__ pend_feat) {
+  for (int k = 0; k <= m; k++) {
+    const size_t row = (size_t)(base + path[k]);
+    const float *src = x + row * d;
+    const float rs = norm_scale(ssq, nt, row, d, eps);
+    float *dst = pend_feat + (size_t)(e * SV_MAX_PENDING + k) * d;
+    for (int i = threadIdx.x * 4; i < d; i += blockDim.x * 4) {
+      const float4 v = *reinterpret_cast<const float4 *>(src + i);
+      const float4 g = *reinterpret_cast<const float4 *>(gain + i);
+      *reinterpret_cast<float4 *>(dst + i) = make_float4(v.x * rs * g.x, v.y * rs * g.y, v.z * rs * g.z, v.w * rs * g.w);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------
 // Relaxed acceptance (Eq. 4) and longest-accepted-path selection, one warp per episode.
 // Node i is accepted iff its parent is accepted and |bin(tok[i]) - bin(g[parent[i]])| <= r
@@ -459,18 +476,26 @@ accept_select_kernel(EpArgs ea, DevTree *trees, EpState *st, const int *__restri
   }
   __syncthreads();
   const int m = s_m;
-  // features (final-norm outputs) of the rows on the path, for the draft model's next call
-  for (int k = 0; k <= m; k++) {
-    const size_t row = (size_t)(base + s_path[k]);
-    const float *src = x + row * d;
-    const float rs = norm_scale(ssq, nt, row, d, eps);
-    float *dst = pend_feat + (size_t)(e * SV_MAX_PENDING + k) * d;
-    for (int i = threadIdx.x * 4; i < d; i += blockDim.x * 4) {
-      const float4 v = *reinterpret_cast<const float4 *>(src + i);
-      const float4 g = *reinterpret_cast<const float4 *>(gain + i);
-      *reinterpret_cast<float4 *>(dst + i) = make_float4(v.x * rs * g.x, v.y * rs * g.y, v.z * rs * g.z, v.w * rs * g.w);
-    }
+  store_path_features(e, base, m, s_path, x, ssq, nt, gain, eps, d, pend_feat);
+}
+
+// The same set-up of the next iteration for a path that another kernel has chosen (verification by random
+// numbers): out_m, out_tok and out_path are given.
+__global__ void __launch_bounds__(128)
+commit_path_kernel(EpArgs ea, EpState *st, const float *__restrict__ x, const float *__restrict__ ssq, int nt,
+                   const float *__restrict__ gain, float eps, int d, float *__restrict__ pend_feat,
+                   const int *__restrict__ out_m, const int *__restrict__ out_tok, const int *__restrict__ out_path) {
+  pdl_launch();
+  pdl_wait();
+  const int e = ea.eps[blockIdx.x], m = min(out_m[blockIdx.x], SV_MAX_DEPTH);
+  const int *ot = out_tok + blockIdx.x * (SV_MAX_DEPTH + 1), *op = out_path + blockIdx.x * (SV_MAX_DEPTH + 1);
+  if (threadIdx.x == 0) {
+    EpState &s = st[e];
+    for (int k = 0; k <= m; k++) s.pending_tok[k] = ot[k];
+    s.root = ot[m];
+    s.n_pending = m + 1;
   }
+  store_path_features(e, ea.row0[blockIdx.x], m, op, x, ssq, nt, gain, eps, d, pend_feat);
 }
 
 // In-place KV compaction: accepted row path[j] moves from slot P + path[j] to slot P + j
