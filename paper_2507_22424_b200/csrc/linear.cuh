@@ -62,13 +62,37 @@ __device__ __forceinline__ float2 get2(const float *p) { return *reinterpret_cas
 __device__ __forceinline__ float2 get2(const bf16 *p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(p)); }
 __device__ __forceinline__ float2 get2(const __half *p) { return __half22float2(*reinterpret_cast<const __half2 *>(p)); }
 
-__device__ __forceinline__ float activate(float v, int act) {
+// FAST: for results that are rounded to 16 bits. exp2 and the reciprocal of the special-function unit (2^-22 relative)
+// in place of expf and a division; tanh through v / (1 + exp(-2z)), which cancels nothing.
+template <bool FAST> __device__ __forceinline__ float sigmoid_times(float v, float z) {
+  if (FAST) {
+    float e, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-1.442695041f * z));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return v * r;
+  }
+  return v / (1.f + expf(-z));
+}
+template <bool FAST, int M> __device__ __forceinline__ void activate(float (&v)[M], int act) {
   switch (act) {
-    case ACT_RELU: return v < 0.f ? 0.f : v;                               // (a NaN stays one)
-    case ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678f));
-    case ACT_GELU_TANH: return 0.5f * v * (1.f + tanhf(0.79788456f * (v + 0.044715f * v * v * v)));
-    case ACT_SILU: return v / (1.f + expf(-v));
-    default: return v;
+    case ACT_RELU:
+#pragma unroll
+      for (int j = 0; j < M; j++) v[j] = v[j] < 0.f ? 0.f : v[j];         // (a NaN stays one)
+      break;
+    case ACT_GELU:
+#pragma unroll
+      for (int j = 0; j < M; j++) v[j] = 0.5f * v[j] * (1.f + erff(v[j] * 0.70710678f));
+      break;
+    case ACT_GELU_TANH:
+      // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (v + 0.044715 v^3)
+#pragma unroll
+      for (int j = 0; j < M; j++) v[j] = sigmoid_times<FAST>(v[j], v[j] * (1.595769122f + 0.0713548163f * v[j] * v[j]));
+      break;
+    case ACT_SILU:
+#pragma unroll
+      for (int j = 0; j < M; j++) v[j] = sigmoid_times<FAST>(v[j], v[j]);
+      break;
+    default: break;
   }
 }
 
@@ -103,52 +127,64 @@ __host__ __device__ constexpr int stage_bytes(int tn) { return W_BYTES + tn * KB
 __host__ __device__ constexpr int stages_of(int tn) { return RING / stage_bytes(tn) < MAX_STAGES ? RING / stage_bytes(tn) : MAX_STAGES; }
 __host__ __device__ constexpr int tmem_cols(int tn) { return tn <= 32 ? 32 : tn <= 64 ? 64 : tn <= 128 ? 128 : 256; }
 
-// Finishes and stores 16 accumulator columns (rows t0 .. t0 + 15 of the chunk) of this lane's output column n: v is
-// the accumulator. In pairs, neighbouring lanes exchange a value each per two rows, so that both store two columns
-// of one row: half as many stores.
-template <int KIND, typename OUT>
-__device__ __forceinline__ void finish16(const Args &a, const uint32_t (&v)[16], int n, int t0, int T, long long row0,
-                                         float sw, float b, const float *s_scale) {
-  OUT *y = static_cast<OUT *>(a.y);
+// The residual of 16 accumulator columns (rows t0 .. t0 + 15 of the chunk) of this lane's output column n, as finish16
+// adds it: asked for ahead of the accumulator, so that the loads are in flight together.
+template <typename OUT>
+__device__ __forceinline__ void residual16(const Args &a, float2 (&r)[8], int n, int t0, int T, long long row0) {
   const OUT *res = static_cast<const OUT *>(a.res);
-  const bool odd = n & 1;
+#pragma unroll
+  for (int p = 0; p < 8; p++) {
+    r[p] = make_float2(0.f, 0.f);
+    if (!res) continue;
+    if (a.pairs) {
+      const int t = t0 + 2 * p + (n & 1), ne = n & ~1;
+      const OUT *q = res + (row0 + t) * a.ldr + ne;
+      if (t < T && ne + 1 < a.N) r[p] = get2(q);
+      else if (t < T && ne < a.N) r[p].x = as_float(*q);
+    } else {
+      const int t = t0 + 2 * p;
+      const OUT *q = res + (row0 + t) * a.ldr + n;
+      if (t < T && n < a.N) r[p].x = as_float(*q);
+      if (t + 1 < T && n < a.N) r[p].y = as_float(q[a.ldr]);
+    }
+  }
+}
+// Finishes and stores these 16 columns: v is the accumulator. In pairs, neighbouring lanes exchange a value each per
+// two rows, so that both store two columns of one row: half as many stores.
+template <int KIND, typename OUT>
+__device__ __forceinline__ void finish16(const Args &a, const uint32_t (&acc)[16], const float2 (&r)[8], int n, int t0, int T,
+                                         long long row0, float sw, float b, const float *s_scale) {
+  constexpr bool FAST = sizeof(OUT) == 2;
+  float v[16];
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) {
+    const float4 sx = *reinterpret_cast<const float4 *>(s_scale + t0 + j);
+    v[j] = fmaf(acc_value<KIND>(acc[j]), sw * sx.x, b);
+    v[j + 1] = fmaf(acc_value<KIND>(acc[j + 1]), sw * sx.y, b);
+    v[j + 2] = fmaf(acc_value<KIND>(acc[j + 2]), sw * sx.z, b);
+    v[j + 3] = fmaf(acc_value<KIND>(acc[j + 3]), sw * sx.w, b);
+  }
+  activate<FAST>(v, a.act);
+  OUT *y = static_cast<OUT *>(a.y);
   if (a.pairs) {
+    const bool odd = n & 1;
     const int ne = n & ~1;
     const bool one = ne < a.N, two = ne + 1 < a.N;
-    float2 rr[8];
+    OUT *q = y + (row0 + t0 + (odd ? 1 : 0)) * a.ldy + ne;
 #pragma unroll
-    for (int p = 0; p < 8; p++) {
-      const int t = t0 + 2 * p + (odd ? 1 : 0);
-      rr[p] = make_float2(0.f, 0.f);
-      if (res && t < T && one) {
-        const OUT *q = res + (row0 + t) * a.ldr + ne;
-        if (two) rr[p] = get2(q);
-        else rr[p].x = as_float(*q);
-      }
-    }
-#pragma unroll
-    for (int p = 0; p < 8; p++) {
-      const float y0 = activate(acc_value<KIND>(v[2 * p]) * (sw * s_scale[t0 + 2 * p]) + b, a.act);
-      const float y1 = activate(acc_value<KIND>(v[2 * p + 1]) * (sw * s_scale[t0 + 2 * p + 1]) + b, a.act);
-      const float other = __shfl_xor_sync(0xffffffffu, odd ? y0 : y1, 1);
-      const int t = t0 + 2 * p + (odd ? 1 : 0);
-      if (t < T && one) {
-        OUT *q = y + (row0 + t) * a.ldy + ne;
-        const float lo = (odd ? other : y0) + rr[p].x, hi = (odd ? y1 : other) + rr[p].y;
+    for (int p = 0; p < 8; p++, q += 2 * a.ldy) {
+      const float other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * p] : v[2 * p + 1], 1);
+      if (t0 + 2 * p + (odd ? 1 : 0) < T && one) {
+        const float lo = (odd ? other : v[2 * p]) + r[p].x, hi = (odd ? v[2 * p + 1] : other) + r[p].y;
         if (two) put2(q, lo, hi);
         else put(q, lo);
       }
     }
   } else {
+    OUT *q = y + (row0 + t0) * a.ldy + n;
 #pragma unroll
-    for (int j = 0; j < 16; j++) {
-      const int t = t0 + j;
-      if (t < T && n < a.N) {
-        float o = activate(acc_value<KIND>(v[j]) * (sw * s_scale[t]) + b, a.act);
-        if (res) o += as_float(res[(row0 + t) * a.ldr + n]);
-        put(y + (row0 + t) * a.ldy + n, o);
-      }
-    }
+    for (int j = 0; j < 16; j++, q += a.ldy)
+      if (t0 + j < T && n < a.N) put(q, v[j] + (j & 1 ? r[j / 2].y : r[j / 2].x));
   }
 }
 
@@ -162,7 +198,7 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   __shared__ __align__(8) uint64_t s_bar[2 * MAX_STAGES + 1];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail, s_done;
-  __shared__ float s_scale[MAX_TN];
+  __shared__ __align__(16) float s_scale[MAX_TN];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stages = stages_of(a.tn), stage = stage_bytes(a.tn);
   const uint32_t bars = smem_u32(s_bar);
@@ -265,10 +301,13 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       for (int t0 = 0; t0 < T; t0 += 16) {
         uint32_t v[16];
         tc_ld16(ta + t0, v);
-        tc_wait_ld();
         if (S == 1) {
-          finish16<KIND, OUT>(a, v, n, t0, T, row0, sw, b, s_scale);
+          float2 r[8];
+          residual16<OUT>(a, r, n, t0, T, row0);
+          tc_wait_ld();
+          finish16<KIND, OUT>(a, v, r, n, t0, T, row0, sw, b, s_scale);
         } else {
+          tc_wait_ld();
 #pragma unroll
           for (int j = 0; j < 16; j++)                         // (the ring is idle: every MMA has read its operands)
             asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + (uint32_t)(((t0 + j) * BM + q * 32 + lane) * 4)), "r"(v[j]) : "memory");
@@ -310,10 +349,10 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         }
         const OUT *res = static_cast<const OUT *>(a.res);
         OUT *y = static_cast<OUT *>(a.y) + (row0 + t) * a.ldy + n;
-        for (int e = 0; e < 2; e++) {
-          v[e] = activate(v[e] * (sw[e] * s_scale[t]) + b[e], a.act);
+        for (int e = 0; e < 2; e++) v[e] = fmaf(v[e], sw[e] * s_scale[t], b[e]);
+        activate<sizeof(OUT) == 2>(v, a.act);
+        for (int e = 0; e < 2; e++)
           if (res && n + e < a.N) v[e] += as_float(res[(row0 + t) * a.ldr + n + e]);
-        }
         if (two && a.pairs) {
           put2(y, v[0], v[1]);
         } else {
@@ -333,6 +372,240 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     while (global_ns() - t0 < 200000ull) __nanosleep(1000);
   }
   if (warp == 1) tc_dealloc(tmem, cols);
+}
+
+// ------------------------------------------------------------------------- many rows
+// Tiles of 256 columns by up to 256 rows, each by a pair of CTAs: one MMA of M = 256 runs on both SMs and reads W (128
+// rows) and X (half the rows) from the shared memory of the CTA that holds them, so that an SM fetches 32 KB per K block
+// where a tile of its own would cost it 48 KB (L2 bounds the products, not the tensor cores). Persistent: a pair takes
+// every n-th tile; the accumulator has two buffers in tensor memory, and eight warps finish one tile while the
+// tensor cores work on the next.
+constexpr int PAIR_THREADS = 320;          // warp 0 copies, warp 1 MMAs (of the pair's first CTA), warps 2-9 epilogue
+constexpr int PAIR_STAGES = 8;
+__host__ __device__ constexpr int pair_stage(int tn) { return W_BYTES + tn / 2 * KBYTES; }
+__host__ __device__ constexpr int pair_stages(int tn) { return RING / pair_stage(tn) < PAIR_STAGES ? RING / pair_stage(tn) : PAIR_STAGES; }
+
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *tm, int x, int y, uint32_t bar, uint64_t pol) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%2, %3}], [%4], %5;"
+      ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(bar), "l"(pol) : "memory");
+}
+template <int KIND>
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
+  if constexpr (KIND == KIND_16)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
+  else if constexpr (KIND == KIND_I8)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
+}
+// The barrier at this offset in both CTAs receives one arrival when every MMA issued so far has finished.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void arrive_peer(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+struct PairTiles {
+  int tiles, chunks, raster;               // tiles of 256 columns, chunks of a.tn rows, chunks side by side
+};
+// Position i of the order in which tiles are taken: groups of `raster` chunks, within a group tile after tile with its
+// chunks side by side, so that what runs at the same time shares W and X in L2.
+__device__ __forceinline__ void tile_at(const PairTiles &p, int i, int &tile, int &chunk) {
+  const int grp = i / (p.raster * p.tiles), in = i - grp * p.raster * p.tiles;
+  const int width = min(p.raster, p.chunks - grp * p.raster);
+  tile = in / width;
+  chunk = grp * p.raster + in - tile * width;
+}
+
+template <int KIND, typename OUT>
+static __global__ void __launch_bounds__(PAIR_THREADS, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const Args a, const PairTiles p) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t s_bar[2 * PAIR_STAGES + 4];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail, s_done[2];
+  __shared__ __align__(16) float s_scale[2][MAX_TN];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int stages = pair_stages(a.tn), stage = pair_stage(a.tn);
+  const uint32_t bars = smem_u32(s_bar);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (PAIR_STAGES + s); };
+  auto acc_bar = [&](int b) { return bars + 8u * (2 * PAIR_STAGES + b); };         // buffer b holds a tile
+  auto free_bar = [&](int b) { return bars + 8u * (2 * PAIR_STAGES + 2 + b); };    // ... has been read by both CTAs
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+  const int total = p.tiles * p.chunks;
+  // a wait that gave up: both CTAs of the pair leave in the same way
+  auto fail = [&](int code) {
+    atomicExch(a.status, code);
+    for (uint32_t r = 0; r < 2; r++)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(&s_fail), r)), "r"(1) : "memory");
+  };
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&tmW);
+    prefetch_tensormap(&tmX);
+    for (int s = 0; s < stages; s++) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; b++) {
+      mbar_init(acc_bar(b), 1);
+      mbar_init(free_bar(b), 16);                              // the epilogue warps of both CTAs
+    }
+    s_fail = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  if (!a.x_scale)
+    for (int t = threadIdx.x; t < 2 * MAX_TN; t += PAIR_THREADS) (&s_scale[0][0])[t] = 1.f;
+  tc_fence_before();
+  __syncthreads();
+  cooperative_groups::this_cluster().sync();                   // the peer's barriers and tensor memory are there too
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  grid_dep_wait();
+  grid_dep_launch();
+
+  if (warp == 0) {
+    const uint64_t pol = policy_evict_last();
+    const bool lead = elect_one();
+    const uint32_t x_bytes = (uint32_t)(a.tn / 2 * KBYTES);
+    int st = 0, ph = 1, n = 0;
+    bool ok = true;
+    for (int i = pair; ok && i < total; i += pairs) {
+      int tile, chunk;
+      tile_at(p, i, tile, chunk);
+      const int yw = tile * 2 * BM + (int)rank * BM, yx = chunk * a.tn + (int)rank * (a.tn / 2);
+      for (int kb = 0; kb < a.KB; kb++, n++) {
+        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(st), ph, a.wait_ns));
+        if (!ok) {
+          if (lead) fail(SV_ERR_LINEAR_EMPTY);
+          break;
+        }
+        if (lead && n != a.withhold - 1) {
+          const uint32_t s = base + st * stage, bar = peer_addr(full_bar(st), 0);
+          if (rank == 0) mbar_expect_tx(full_bar(st), 2 * (W_BYTES + x_bytes));
+          tma_load_pair(s, &tmW, kb * KBYTES, yw, bar, pol);
+          tma_load_pair(s + W_BYTES, &tmX, kb * KBYTES, yx, bar, pol);
+        }
+        __syncwarp();
+        if (++st == stages) {
+          st = 0;
+          ph ^= 1;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const bool lead = elect_one();
+      int st = 0, ph = 0, buf = 0, fph = 1;
+      bool ok = true;
+      for (int i = pair; ok && i < total; i += pairs) {
+        ok = __all_sync(0xffffffffu, mbar_wait(free_bar(buf), fph, a.wait_ns));
+        if (!ok) {
+          if (lead) fail(SV_ERR_LINEAR_ACC);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d = tmem + (uint32_t)(buf * MAX_TN);
+        for (int kb = 0; kb < a.KB; kb++) {
+          ok = __all_sync(0xffffffffu, mbar_wait(full_bar(st), ph, a.wait_ns));
+          if (!ok) {
+            if (lead) fail(SV_ERR_LINEAR_FULL);
+            break;
+          }
+          tc_fence_after();
+          const uint64_t ad = smem_desc(base + st * stage), bd = smem_desc(base + st * stage + W_BYTES);
+          if (lead) {
+#pragma unroll
+            for (int k = 0; k < KBYTES / 32; k++) mma_pair<KIND>(d, ad + 2 * k, bd + 2 * k, a.idesc, kb > 0 || k > 0);
+            commit_pair(empty_bar(st));
+            if (kb == a.KB - 1) commit_pair(acc_bar(buf));
+          }
+          __syncwarp();
+          if (++st == stages) {
+            st = 0;
+            ph ^= 1;
+          }
+        }
+        if (++buf == 2) {
+          buf = 0;
+          fph ^= 1;
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int et = threadIdx.x - 64, q = warp & 3, half = (warp - 2) >> 2, cols = a.tn / 2;
+    int buf = 0, ph = 0;
+    for (int i = pair; i < total; i += pairs) {
+      int tile, chunk;
+      tile_at(p, i, tile, chunk);
+      const long long row0 = (long long)chunk * a.tn;
+      const int T = min(a.T - chunk * a.tn, a.tn), n = tile * 2 * BM + (int)rank * BM + q * 32 + lane;
+      const float sw = a.w_scale && n < a.N ? a.w_scale[n] : 1.f, b = a.bias && n < a.N ? a.bias[n] : 0.f;
+      if (a.x_scale && et < a.tn) s_scale[buf][et] = et < T ? a.x_scale[row0 + et] : 1.f;
+      if (et == 0) {
+        const bool ok = mbar_wait(acc_bar(buf), ph, a.wait_ns);
+        s_done[buf] = ok;
+        if (!ok) fail(SV_ERR_LINEAR_ACC);
+      }
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (!s_done[buf]) break;
+      tc_fence_after();
+      const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN);
+      const int t_end = min((half + 1) * cols, T);
+      for (int t0 = half * cols; t0 < t_end; t0 += 16) {
+        uint32_t v[16];
+        tc_ld16(ta + t0, v);
+        float2 r[8];
+        residual16<OUT>(a, r, n, t0, T, row0);
+        tc_wait_ld();
+        finish16<KIND, OUT>(a, v, r, n, t0, T, row0, sw, b, s_scale[buf]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_peer(peer_addr(free_bar(buf), 0));
+      if (++buf == 2) {
+        buf = 0;
+        ph ^= 1;
+      }
+    }
+    __syncwarp();
+  }
+  // nobody leaves while the pair's MMAs may read its shared memory or its peer may signal it
+  tc_fence_before();
+  __syncthreads();
+  cooperative_groups::this_cluster().sync();
+  tc_fence_after();
+  if (s_fail) {
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 200000ull) __nanosleep(1000);
+    cooperative_groups::this_cluster().sync();                 // (the flag is the same in both CTAs)
+  }
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------- host side

@@ -107,21 +107,62 @@ const Fit *cluster_fit() {
   return &f;
 }
 
+// How a call is cut. pair: tiles of 256 columns by pairs of CTAs; else tiles of 128 columns by clusters of S CTAs.
+struct Plan {
+  bool pair;
+  int tn, tiles, chunks, S, grid;
+};
+Plan plan_linear(int T, int N, int KB, const Fit *fit) {
+  Plan best = {};
+  // few rows: one pass over W, every K block by one CTA; as many slices as run at once, four K blocks each at least
+  Plan p = {};
+  p.tiles = (N + linear::BM - 1) / linear::BM;
+  p.chunks = (T + linear::MAX_TN - 1) / linear::MAX_TN;
+  p.tn = ((T + p.chunks - 1) / p.chunks + 15) / 16 * 16;
+  p.chunks = (T + p.tn - 1) / p.tn;
+  p.S = 1;
+  for (int s = 2; fit && s <= linear::MAX_S; s++)
+    if ((long long)fit->clusters[s] >= (long long)p.tiles * p.chunks && KB / s >= 4) p.S = s;
+  best = p;
+  if (T > 128 && fit && fit->clusters[2] > 0) {
+    const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
+    double cost = 1e30;
+    const int cmin = (T + linear::MAX_TN - 1) / linear::MAX_TN;
+    for (int c = cmin; c <= 4 * cmin + 4 && c <= T; c++) {
+      const int tn = ((T + c - 1) / c + 31) / 32 * 32;
+      if (tn > linear::MAX_TN || tn < 64) continue;
+      const int chunks = (T + tn - 1) / tn;
+      const long long waves = ((long long)tiles * chunks + pairs - 1) / pairs;
+      const double k = waves * (double)(KB * (tn + 32) + 1000);
+      if (k < cost) {
+        cost = k;
+        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2};
+      }
+    }
+  }
+  return best;
+}
+
 template <int KIND, typename OUT>
-int linear_launch(const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, int tiles, int chunks, int S, void *stream) {
-  auto kernel = linear::linear_slice_kernel<KIND, OUT>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, linear::SMEM) != cudaSuccess) {
+int linear_launch(const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, const Plan &p, void *stream) {
+  auto slice = linear::linear_slice_kernel<KIND, OUT>;
+  auto pair = linear::linear_pair_kernel<KIND, OUT>;
+  if ((p.pair ? cudaFuncSetAttribute(pair, cudaFuncAttributeMaxDynamicSharedMemorySize, linear::SMEM)
+              : cudaFuncSetAttribute(slice, cudaFuncAttributeMaxDynamicSharedMemorySize, linear::SMEM)) != cudaSuccess) {
     cudaGetLastError();
     return SPECVLA_ERR_CUDA;
   }
-  return launch(kernel, dim3(tiles * S, chunks), dim3(linear::THREADS), linear::SMEM, S, stream, mw, mx, a, S);
+  if (p.pair)
+    return launch(pair, dim3(p.grid), dim3(linear::PAIR_THREADS), linear::SMEM, 2, stream, mw, mx, a,
+                  linear::PairTiles{p.tiles, p.chunks, 8});
+  return launch(slice, dim3(p.tiles * p.S, p.chunks), dim3(linear::THREADS), linear::SMEM, p.S, stream, mw, mx, a, p.S);
 }
 template <int KIND>
-int linear_out(int out_type, const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, int tiles, int chunks, int S, void *stream) {
+int linear_out(int out_type, const CUtensorMap &mw, const CUtensorMap &mx, const linear::Args &a, const Plan &p, void *stream) {
   switch (out_type) {
-    case SPECVLA_F32: return linear_launch<KIND, float>(mw, mx, a, tiles, chunks, S, stream);
-    case SPECVLA_BF16: return linear_launch<KIND, bf16>(mw, mx, a, tiles, chunks, S, stream);
-    default: return linear_launch<KIND, __half>(mw, mx, a, tiles, chunks, S, stream);
+    case SPECVLA_F32: return linear_launch<KIND, float>(mw, mx, a, p, stream);
+    case SPECVLA_BF16: return linear_launch<KIND, bf16>(mw, mx, a, p, stream);
+    default: return linear_launch<KIND, __half>(mw, mx, a, p, stream);
   }
 }
 
@@ -190,26 +231,19 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   g_linear_wait_ns = gemm_tc::WAIT_LIMIT_NS;                     // the test hook holds for one call
   g_linear_withhold = 0;
   const int kind = l->type == SPECVLA_I8 ? linear::KIND_I8 : l->type == SPECVLA_E4M3 ? linear::KIND_E4M3 : linear::KIND_16;
-  const int tiles = (l->N + linear::BM - 1) / linear::BM;
-  int chunks = (l->T + linear::MAX_TN - 1) / linear::MAX_TN;
-  a.tn = ((l->T + chunks - 1) / chunks + 15) / 16 * 16;
-  chunks = (l->T + a.tn - 1) / a.tn;
-  if (chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
-  // K slices: as many as run at once, four K blocks each at least
-  int S = 1;
-  const Fit *fit = cluster_fit();
-  for (int s = 2; fit && s <= linear::MAX_S; s++)
-    if ((long long)fit->clusters[s] >= (long long)tiles * chunks && a.KB / s >= 4) S = s;
-  a.idesc = linear::make_idesc(kind, l->type == SPECVLA_BF16, linear::BM, a.tn);
+  const Plan p = plan_linear(l->T, l->N, a.KB, cluster_fit());
+  if (p.chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
+  a.tn = p.tn;
+  a.idesc = linear::make_idesc(kind, l->type == SPECVLA_BF16, p.pair ? 2 * linear::BM : linear::BM, a.tn);
   CUtensorMap mw, mx;
-  if (!linear::make_map(&mw, l->W, l->N, bytes, ldw, linear::BM) || !linear::make_map(&mx, l->X, l->T, bytes, ldx, a.tn)) {
+  if (!linear::make_map(&mw, l->W, l->N, bytes, ldw, linear::BM) || !linear::make_map(&mx, l->X, l->T, bytes, ldx, p.pair ? a.tn / 2 : a.tn)) {
     cudaGetLastError();
     return SPECVLA_ERR_CUDA;
   }
   switch (kind) {
-    case linear::KIND_16: return linear_out<linear::KIND_16>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
-    case linear::KIND_I8: return linear_out<linear::KIND_I8>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
-    default: return linear_out<linear::KIND_E4M3>(l->out_type, mw, mx, a, tiles, chunks, S, stream);
+    case linear::KIND_16: return linear_out<linear::KIND_16>(l->out_type, mw, mx, a, p, stream);
+    case linear::KIND_I8: return linear_out<linear::KIND_I8>(l->out_type, mw, mx, a, p, stream);
+    default: return linear_out<linear::KIND_E4M3>(l->out_type, mw, mx, a, p, stream);
   }
 }
 

@@ -28,7 +28,7 @@ namespace sampled {
 constexpr int SUB = 512;                  // ids that one warp sums
 constexpr int STATS_THREADS = 256;
 constexpr int WALK_THREADS = 512;
-constexpr int CLUSTER = 8;
+constexpr int CLUSTER = 8;                // largest
 constexpr int MAX_IDS = 1 << 20;          // ids that may take part
 inline int pieces_of(int ids) { return (ids + SUB - 1) / SUB; }
 
@@ -59,36 +59,53 @@ template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f<bf16>(bf16 v) { return __bfloat162float(v); }
 template <> __device__ __forceinline__ float to_f<__half>(__half v) { return __half2float(v); }
 
-// 2^(i / 64) for the exponential below, filled by the kernel's first threads.
+// 2^(i / 64), copied to shared memory by a kernel's first threads.
+static __device__ const double EXP2_64[64] = {
+    1, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284,
+    1.0442737824274138, 1.0556451783605572, 1.0671404006768237, 1.0787607977571199,
+    1.0905077326652577, 1.1023825833078409, 1.1143867425958924, 1.1265216186082418,
+    1.1387886347566916, 1.1511892299529827, 1.1637248587775775, 1.1763969916502812,
+    1.189207115002721, 1.2021567314527031, 1.215247359980469, 1.22848053610687,
+    1.241857812073484, 1.2553807570246911, 1.2690509571917332, 1.2828700160787783,
+    1.2968395546510096, 1.3109612115247644, 1.3252366431597413, 1.3396675240533029,
+    1.3542555469368927, 1.3690024229745905, 1.383909881963832, 1.3989796725383112,
+    1.4142135623730951, 1.42961333839197, 1.4451808069770467, 1.460917794180647,
+    1.4768261459394993, 1.4929077282912648, 1.5091644275934228, 1.5255981507445384,
+    1.5422108254079407, 1.5590044002378369, 1.5759808451078865, 1.593142151342267,
+    1.6104903319492543, 1.6280274218573478, 1.6457554781539649, 1.6636765803267364,
+    1.681792830507429, 1.7001063537185235, 1.7186192981224779, 1.7373338352737062,
+    1.7562521603732995, 1.7753764925265212, 1.7947090750031072, 1.8142521755003989,
+    1.8340080864093424, 1.8539791250833855, 1.8741676341103, 1.8945759815869656,
+    1.9152065613971474, 1.9360617934922943, 1.9571441241754002, 1.9784560263879509,
+};
 struct ExpTable { double t[64]; };
 __device__ __forceinline__ void fill(ExpTable &tab) {
-  if (threadIdx.x < 64) tab.t[threadIdx.x] = exp2((double)threadIdx.x * 0.015625);
+  if (threadIdx.x < 64) tab.t[threadIdx.x] = EXP2_64[threadIdx.x];
 }
-// exp(x) for x <= 0: x = n ln2 / 64 + r, |r| <= ln2 / 128, exp(x) = 2^(n / 64) (1 + r + ... + r^5 / 120); the first
-// term left out is below 4e-17. Below -700: 0.
-__device__ __forceinline__ double exp_neg(double x, const ExpTable &tab) {
-  constexpr double INV = 92.332482616893656877;              // 64 / ln 2
-  constexpr double LN2_HI = 0.010830424667801708, LN2_LO = 2.8447437476627285e-11;   // ln 2 / 64 in two parts
-  constexpr double MAGIC = 6755399441055744.0;               // 1.5 * 2^52
-  const double m = fma(x, INV, MAGIC);
-  const int n = (int)(unsigned)__double_as_longlong(m);
-  const double nd = m - MAGIC;
-  const double r = fma(nd, -LN2_LO, fma(nd, -LN2_HI, x));
-  double p = fma(r, 1.0 / 120, 1.0 / 24);
-  p = fma(p, r, 1.0 / 6);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  const double t = tab.t[n & 63];
-  const double s = __hiloint2double(__double2hiint(t) + ((n >> 6) << 20), __double2loint(t));
-  return x < -700.0 ? 0.0 : p * s;
-}
-// exp((z - max) / temperature), 0 for a NaN; max itself (an infinite one too) has 1.
-__device__ __forceinline__ double weight(float z, float zmax, double inv_t, const ExpTable &tab) {
-  if (z == zmax) return 1.0;
-  const double x = ((double)z - (double)zmax) * inv_t;
-  return x < 0.0 ? exp_neg(x, tab) : 0.0;                     // (NaN compares false)
-}
+__device__ __forceinline__ double exp_factor(float temperature) { return 92.332482616893657 / (double)temperature; }
+// Weights of one row: exp((z - zmax) / temperature) = 2^(y / 64) with y = (z - zmax) 64 / (ln 2 temperature) = n + r,
+// n whole, |r| <= 1/2: a table entry, a power of two and a polynomial of degree 4 in r (the first term left out is
+// below 4e-14). Ten 64-bit operations with the sum. zmax has 1, an infinite one too; a NaN, and what lies below e^-700, 0.
+struct RowExp {
+  float zmax, low;
+  double k;
+  __device__ __forceinline__ RowExp(float zm, float temperature, double k_)
+      : zmax(zm), low(zm - 700.f * temperature), k(k_) {}
+  __device__ __forceinline__ double operator()(float z, const ExpTable &tab) const {
+    constexpr double MAGIC = 6755399441055744.0;               // 1.5 * 2^52
+    const double d = (double)z - (double)zmax;
+    const double m = fma(d, k, MAGIC);
+    const int n = __double2loint(m);
+    const double r = fma(d, k, MAGIC - m);
+    double p = fma(r, 5.7328516886404019e-10, 2.1173137155464776e-07);
+    p = fma(p, r, 5.86490495505617e-05);
+    p = fma(p, r, 0.010830424696249145);
+    p = fma(p, r, 1.0);
+    const double t = tab.t[n & 63];
+    p *= __hiloint2double(__double2hiint(t) + ((n >> 6) << 20), __double2loint(t));
+    return z == zmax ? 1.0 : z > low ? p : 0.0;
+  }
+};
 
 __device__ __forceinline__ double warp_sum64(double v) {
 #pragma unroll
@@ -141,11 +158,11 @@ static __global__ void __launch_bounds__(STATS_THREADS) stats_kernel(const Args 
 #pragma unroll
   for (int k = 0; k < 16; k++) m = fmaxf(m, z[k]);             // (a NaN loses)
   m = warp_max(m);
-  const double inv_t = 1.0 / (double)a.temperature;
+  const RowExp weight(m, a.temperature, exp_factor(a.temperature));
   double s = 0.0;
   if (m > -INFINITY) {
 #pragma unroll
-    for (int k = 0; k < 16; k++) s += weight(z[k], m, inv_t, tab);
+    for (int k = 0; k < 16; k++) s += weight(z[k], tab);
   }
   s = warp_sum64(s);
   if (lane == 0) {
@@ -155,60 +172,30 @@ static __global__ void __launch_bounds__(STATS_THREADS) stats_kernel(const Args 
 }
 
 struct Walk {
-  float zmax[SV_MAX_TREE];                // of every row
+  float zmax[SV_MAX_TREE];                // of a row with children
   double z[SV_MAX_TREE];                  // its sum of weights; 0: nothing to draw from, the lowest id has all
-  double w[SV_MAX_TREE];                  // weight of the row's token in its parent's row
+  double w[SV_MAX_TREE];                  // weight of the row's token in its parent's row (PROBS: over its sum)
   float q[SV_MAX_TREE], u[SV_MAX_TREE];
   int tok[SV_MAX_TREE], parent[SV_MAX_TREE];
+  int inner[SV_MAX_TREE];                 // the row has children
+  int yes[SV_MAX_TREE];                   // no PROBS: the row is accepted if the walk comes to it
+  int again[SV_MAX_TREE];                 // no PROBS: an elder sibling has the same token
   int path[SV_MAX_TREE];
-  int refused[SV_MAX_TREE];                // tokens refused at the row where the walk stands, each once
+  int refused[SV_MAX_TREE];               // tokens refused at the row where the walk ends, each once
   int n_refused, cur, next, m, want;      // want: the walk waits for a pass over the vocabulary
   double beta, S;
   double part[2][CLUSTER];                // sums of the cluster's CTAs, by turns
   double warp_part[WALK_THREADS / 32];
 };
 
-// The token at `target` within a piece that begins at the cumulative sum `before` (whole warp): the first id
-// whose cumulative weight exceeds it, else the last one that has any.
-__device__ __forceinline__ int search_piece(double before, double target, int first, const double (&wt)[16]) {
-  const int lane = threadIdx.x & 31;
-  int last = -1;
-#pragma unroll
-  for (int j = 0; j < 4; j++) {
-    const double mine = ((wt[4 * j] + wt[4 * j + 1]) + wt[4 * j + 2]) + wt[4 * j + 3];
-    double incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const double up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
-    }
-    double c = before + (incl - mine);
-    int found = -1, any = -1;
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-      c += wt[4 * j + e];
-      if (wt[4 * j + e] > 0.0) {
-        any = first + 128 * j + 4 * lane + e;
-        if (found < 0 && c > target) found = any;
-      }
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
-    if (hit) return __shfl_sync(0xffffffffu, found, __ffs(hit) - 1);
-    const unsigned some = __ballot_sync(0xffffffffu, any >= 0);
-    if (some) last = __shfl_sync(0xffffffffu, any, 31 - __clz(some));
-    before += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  return last;
-}
-
-// The piece at `target` of n sums (whole warp): sums[k] is given by `at`; returns the piece, or the last one that has
-// any weight, and the cumulative sum before it. -1: none has.
-template <typename F> __device__ __forceinline__ int search_sums(int n, double target, F at, double *before) {
+// The piece at `target` of n sums (whole warp), and the cumulative sum before it; the last piece that has any weight
+// where none reaches it, -1: none has.
+__device__ __forceinline__ int search_sums(int n, double target, const double *sums, double *before) {
   const int lane = threadIdx.x & 31;
   double base = 0.0, last_base = 0.0;
   int last = -1;
   for (int k0 = 0; k0 < n; k0 += 32) {
-    const double v = k0 + lane < n ? at(k0 + lane) : 0.0;
+    const double v = k0 + lane < n ? sums[k0 + lane] : 0.0;
     double incl = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -233,48 +220,100 @@ template <typename F> __device__ __forceinline__ int search_sums(int n, double t
   *before = last_base;
   return last;
 }
+// The same among 16 consecutive ids a lane, which begin at the cumulative sum `before`: the first id whose cumulative
+// weight exceeds `target`, else the last that has any.
+__device__ __forceinline__ int search_ids(double before, double target, int first, const double (&wt)[16]) {
+  const int lane = threadIdx.x & 31;
+  double mine = 0.0;
+#pragma unroll
+  for (int e = 0; e < 16; e++) mine += wt[e];
+  double incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  double c = before + (incl - mine);
+  int found = -1, any = -1;
+#pragma unroll
+  for (int e = 0; e < 16; e++) {
+    c += wt[e];
+    if (wt[e] > 0.0) {
+      any = first + 16 * lane + e;
+      if (found < 0 && c > target) found = any;
+    }
+  }
+  const unsigned hit = __ballot_sync(0xffffffffu, found >= 0);
+  if (hit) return __shfl_sync(0xffffffffu, found, __ffs(hit) - 1);
+  const unsigned some = __ballot_sync(0xffffffffu, any >= 0);
+  return some ? __shfl_sync(0xffffffffu, any, 31 - __clz(some)) : -1;
+}
 
 // Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends.
 template <typename T, bool PROBS, bool CTX>
-static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args a, const EpArgs ea) {
+static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args a, const EpArgs ea) {
   namespace cg = cooperative_groups;
   __shared__ ExpTable tab;
   __shared__ Walk w;
   extern __shared__ double s_sub[];
   fill(tab);
   if (PROBS) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (that every CTA has started)
-  __syncthreads();
-  pdl_wait();
-  pdl_launch();
-  const int rank = PROBS ? (int)(blockIdx.x % CLUSTER) : 0, ranks = PROBS ? CLUSTER : 1;
-  const int seq = PROBS ? (int)(blockIdx.x / CLUSTER) : (int)blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int WARPS = WALK_THREADS / 32;
+  if (tid < SV_MAX_TREE) w.inner[tid] = 0;
+  int rank = 0, ranks = 1;
+  if (PROBS) {
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+  }
+  const int seq = (int)blockIdx.x / ranks;
+  const double factor = exp_factor(a.temperature);
+  pdl_wait();
+  pdl_launch();
   const DevTree *tr = CTX ? a.trees + ea.eps[seq] : nullptr;
   const long long row0 = CTX ? ea.row0[seq] : (long long)seq * a.rows;
   const int n = CTX ? tr->n_rows : a.n_rows ? min(max(a.n_rows[seq], 1), a.rows) : a.rows;
   const int width = a.hi - a.lo;
-  const double inv_t = 1.0 / (double)a.temperature;
   auto logits_of = [&](int i) { return static_cast<const T *>(a.logits) + (row0 + i) * a.ld + a.lo; };
   auto probs_of = [&](int i) { return a.probs + (row0 + i) * a.ld_probs + a.lo; };
-
-  // ---- all rows: maximum and sum from the pieces, a warp per row
-  for (int i = tid; i < n; i += WALK_THREADS) {
-    w.tok[i] = CTX ? tr->tok[i] : a.tokens[row0 + i];
-    w.parent[i] = CTX ? tr->parent[i] : a.parent[row0 + i];
-    w.u[i] = a.u[row0 + i];
-  }
-  for (int i = warp; i < n; i += WARPS) {
-    const float *sm = a.sub_max + (size_t)(row0 + i) * a.n_sub;
-    const double *su = a.sub_sum + (size_t)(row0 + i) * a.n_sub;
+  auto maxima_of = [&](int i) { return a.sub_max + (size_t)(row0 + i) * a.n_sub; };
+  auto sums_of = [&](int i) { return a.sub_sum + (size_t)(row0 + i) * a.n_sub; };
+  auto row_max = [&](const float *sm) {                          // (whole warp)
     float m = -INFINITY;
     for (int k = lane; k < a.n_sub; k += 32) m = fmaxf(m, sm[k]);
-    m = warp_max(m);
-    __syncwarp();
+    return warp_max(m);
+  };
+
+  // ---- the tree; a thread keeps its row's parent and token
+  __syncthreads();
+  int my_parent = -1, my_x = -1;
+  float my_z = 0.f, my_q = 0.f;
+  if (tid < n) {
+    my_x = (int)((unsigned)(CTX ? tr->tok[tid] : a.tokens[row0 + tid]) - (unsigned)a.lo);
+    my_parent = CTX ? tr->parent[tid] : a.parent[row0 + tid];
+    if (tid == 0 || my_parent < 0 || my_parent >= tid) my_parent = -1;   // no row's child
+    w.u[tid] = a.u[row0 + tid];
+    w.tok[tid] = my_x;
+    w.parent[tid] = my_parent;
+    if (my_parent >= 0) w.inner[my_parent] = 1;
+  }
+  const bool inside = my_parent >= 0 && my_x >= 0 && my_x < width;
+  if (inside) {
+    my_z = to_f(logits_of(my_parent)[my_x]);
+    if (PROBS) my_q = fmaxf(probs_of(my_parent)[my_x], 0.f);
+  }
+  __syncthreads();
+  // ---- rows with children: maximum and sum from the pieces, a warp per row
+  for (int i = warp; i < n; i += WARPS) {
+    if (!w.inner[i]) continue;
+    const float *sm = maxima_of(i);
+    const double *su = sums_of(i);
+    const float m = row_max(sm);
+    const RowExp weight(m, a.temperature, factor);
     double z = 0.0;
     if (m > -INFINITY)
       for (int k = lane; k < a.n_sub; k += 32)
-        if (sm[k] > -INFINITY) z += su[k] * weight(sm[k], m, inv_t, tab);
+        if (sm[k] > -INFINITY) z += su[k] * weight(sm[k], tab);
     z = warp_sum64(z);
     if (lane == 0) w.zmax[i] = m, w.z[i] = z;
   }
@@ -283,78 +322,98 @@ static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args
     w.beta = 0.0, w.S = 1.0;
   }
   __syncthreads();
-  // weight (in units of the row's sum) of id x of row i
-  auto p_of = [&](int i, float z, int x) -> double {
-    if (!(w.z[i] > 0.0)) return x == 0 ? 1.0 : 0.0;
-    return weight(z, w.zmax[i], inv_t, tab) / w.z[i];
+  // weight of id x of a row with children, and the sum of its row
+  auto weight_of = [&](int i, float z, int x) {
+    return w.z[i] > 0.0 ? RowExp(w.zmax[i], a.temperature, factor)(z, tab) : x == 0 ? 1.0 : 0.0;
   };
-  for (int i = 1 + tid; i < n; i += WALK_THREADS) {
-    const int p = w.parent[i], x = w.tok[i] - a.lo;
-    const bool ok = p >= 0 && p < i && x >= 0 && x < width;
-    w.w[i] = ok ? p_of(p, to_f(logits_of(p)[x]), x) : 0.0;
-    w.q[i] = PROBS && ok ? fmaxf(probs_of(p)[x], 0.f) : 0.f;
-    if (!ok && (p < 0 || p >= i)) w.parent[i] = -1;              // no row's child
+  auto sum_of = [&](int i) { return w.z[i] > 0.0 ? w.z[i] : 1.0; };
+  if (tid < n) {
+    const double v = inside ? weight_of(my_parent, my_z, my_x) : 0.0;
+    w.w[tid] = PROBS ? (inside ? v / sum_of(my_parent) : 0.0) : v;
+    w.q[tid] = my_q;
+    if (!PROBS) {
+      bool again = false;
+      for (int j = 1; j < tid; j++) again |= w.parent[j] == my_parent && w.tok[j] == my_x;
+      w.again[tid] = again;
+    }
   }
   __syncthreads();
-
+  if (!PROBS) {
+    // what is left of the parent's row when the walk comes to this child: every child is decided at once
+    if (tid < n) {
+      bool yes = false;
+      if (inside && !w.again[tid]) {
+        double S = sum_of(my_parent);
+        for (int j = 1; j < tid; j++)
+          if (w.parent[j] == my_parent && !w.again[j]) S -= w.w[j];
+        yes = w.w[tid] > 0.0 && (double)w.u[tid] * S < w.w[tid];
+      }
+      w.yes[tid] = yes;
+    }
+    __syncthreads();
+  }
   if (PROBS) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
   // ---- the walk: a warp runs it from shared memory, everybody joins for a pass over the vocabulary
   int turn = 0;
   for (;;) {
     if (warp == 0) {
-      int cur = w.cur, m = w.m, nref = w.n_refused;
-      double beta = w.beta, S = w.S;
-      int want = 0;
-      for (int i0 = w.next; i0 < n && !want;) {
-        const int i = i0 + lane;
-        const unsigned kids = __ballot_sync(0xffffffffu, i < n && w.parent[i] == cur);
-        if (!kids) {
-          i0 += 32;
-          continue;
-        }
-        const int c = i0 + __ffs(kids) - 1;
-        i0 = c + 1;
-        const int x = w.tok[c] - a.lo;
-        bool take;
-        if (PROBS) {
+      int cur = w.cur, m = w.m;
+      if constexpr (PROBS) {
+        double beta = w.beta, S = w.S;
+        int want = 0, i0 = w.next;
+        while (i0 < n && !want) {
+          const unsigned kids = __ballot_sync(0xffffffffu, i0 + lane < n && w.parent[i0 + lane] == cur);
+          if (!kids) {
+            i0 += 32;
+            continue;
+          }
+          const int c = i0 + __ffs(kids) - 1;
+          i0 = c + 1;
           const double q = w.q[c], r = w.w[c] - beta * q;
-          take = r > 0.0 && (double)w.u[c] * q * S < r;
-        } else {
-          bool twice = false;
-          for (int k = lane; k < nref; k += 32) twice |= w.refused[k] == x;
-          twice = __any_sync(0xffffffffu, twice);
-          const double r = twice ? 0.0 : w.w[c];
-          take = r > 0.0 && (double)w.u[c] * S < r;
-          if (!take && !twice && x >= 0 && x < width) {
-            __syncwarp();
-            if (lane == 0) w.refused[nref] = x;
-            nref++;
-            S -= r;
-            __syncwarp();
+          if (r > 0.0 && (double)w.u[c] * q * S < r) {
+            cur = c;
+            m++;
+            beta = 0.0, S = 1.0;
+            if (lane == 0) w.path[m] = c;
+          } else {
+            beta += S;
+            want = 1;                                            // the sum of what is left
           }
         }
-        if (take) {
-          cur = c;
+        if (lane == 0) w.cur = cur, w.m = m, w.next = i0, w.beta = beta, w.S = S, w.want = want;
+      } else {
+        for (int i0 = 1; i0 < n;) {
+          const unsigned kids = __ballot_sync(0xffffffffu, i0 + lane < n && w.parent[i0 + lane] == cur && w.yes[i0 + lane]);
+          if (!kids) {
+            i0 += 32;
+            continue;
+          }
+          cur = i0 + __ffs(kids) - 1;
+          i0 = cur + 1;
           m++;
-          nref = 0;
-          beta = 0.0, S = 1.0;
-          if (lane == 0) w.path[m] = c;
-        } else if (PROBS) {
-          beta += S;
-          want = 1;                                              // S of the next beta
+          if (lane == 0) w.path[m] = cur;
         }
-        if (lane == 0) w.next = i0;
+        // the children refused there
+        int nref = 0;
+        for (int i0 = cur + 1; i0 < n; i0 += 32) {
+          const int i = i0 + lane;
+          const bool no = i < n && w.parent[i] == cur && !w.again[i] && w.tok[i] >= 0 && w.tok[i] < width;
+          const unsigned all = __ballot_sync(0xffffffffu, no);
+          if (no) w.refused[nref + __popc(all & ((1u << lane) - 1))] = w.tok[i];
+          nref += __popc(all);
+        }
+        if (lane == 0) w.cur = cur, w.m = m, w.n_refused = nref;
       }
-      __syncwarp();
-      if (lane == 0) w.cur = cur, w.m = m, w.n_refused = nref, w.beta = beta, w.S = S, w.want = want;
     }
     __syncthreads();
     if (!PROBS || !w.want) break;
     if constexpr (PROBS) {
       // S = sum of max(p - beta q, 0): pieces go round the cluster's warps; their sums stay for the search
       const int cur = w.cur;
-      const double beta = w.beta, inv_z = w.z[cur] > 0.0 ? 1.0 / w.z[cur] : 0.0;
+      const bool none = !(w.z[cur] > 0.0);
+      const double beta = w.beta, inv_z = 1.0 / sum_of(cur);
+      const RowExp weight(w.zmax[cur], a.temperature, factor);
       const T *z0 = logits_of(cur);
       const float *q0 = probs_of(cur);
       const bool vz = aligned4(z0), vq = aligned4(q0);
@@ -367,7 +426,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args
 #pragma unroll
         for (int e = 0; e < 16; e++) {
           const int x = k * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
-          const double p = inv_z > 0.0 ? weight(z[e], w.zmax[cur], inv_t, tab) * inv_z : x == 0 ? 1.0 : 0.0;
+          const double p = none ? (x == 0 ? 1.0 : 0.0) : weight(z[e], tab) * inv_z;
           if (x < width) s += fmax(p - beta * (double)fmaxf(q[e], 0.f), 0.0);
         }
         s = warp_sum64(s);
@@ -376,13 +435,13 @@ static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args
       }
       if (lane == 0) w.warp_part[warp] = mine;
       __syncthreads();
-      if (tid == 0) {
+      if (tid < ranks) {
         double s = 0.0;
         for (int k = 0; k < WARPS; k++) s += w.warp_part[k];
-        cg::cluster_group cl = cg::this_cluster();
-        for (int k = 0; k < ranks; k++) *cl.map_shared_rank(&w.part[turn][rank], k) = s;
+        *cg::this_cluster().map_shared_rank(&w.part[turn][rank], tid) = s;
       }
-      cg::this_cluster().sync();
+      if (ranks > 1) cg::this_cluster().sync();
+      else __syncthreads();
       if (tid == 0) {
         double s = 0.0;
         for (int k = 0; k < ranks; k++) s += w.part[turn][k];
@@ -393,10 +452,10 @@ static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args
     }
   }
 
-  // ---- the token after the path
+  // ---- the token after the path, from what is left of its last row
   const int cur = w.cur, m = w.m;
   const bool residual = PROBS && w.beta > 0.0 && w.S > 0.0;      // (the last pass was made with this beta)
-  if constexpr (PROBS) {
+  if (PROBS && ranks > 1) {
     // every CTA has its own pieces' sums: the first one collects them
     cg::cluster_group cl = cg::this_cluster();
     if (residual && rank != 0)
@@ -405,85 +464,81 @@ static __global__ void __launch_bounds__(WALK_THREADS, 1) walk_kernel(const Args
     cl.sync();
     if (rank != 0) return;
   }
-  const bool none = !(w.z[cur] > 0.0);
+  const float *sm = maxima_of(cur);
+  const double *su = sums_of(cur);
+  const float zm = w.inner[cur] ? w.zmax[cur] : row_max(sm);
+  const RowExp weight(zm, a.temperature, factor);
+  const bool none = !(zm > -INFINITY);
+  auto plain_sums = [&](int first, int step) {
+    for (int k = first; k < a.n_sub; k += step) s_sub[k] = sm[k] > -INFINITY ? su[k] * weight(sm[k], tab) : 0.0;
+  };
   if (!residual) {
-    // what is left is p, without the refused tokens: the sums of the pieces that hold one are made again
-    const float zm = w.zmax[cur];
-    const float *sm = a.sub_max + (size_t)(row0 + cur) * a.n_sub;
-    const double *su = a.sub_sum + (size_t)(row0 + cur) * a.n_sub;
-    for (int k = tid; k < a.n_sub; k += WALK_THREADS) {
-      const float km = sm[k];
-      s_sub[k] = km > -INFINITY ? su[k] * weight(km, zm, inv_t, tab) : 0.0;
-    }
-    __syncthreads();
-    if (!PROBS) {
-      for (int k = warp; k < w.n_refused; k += WARPS) {
-        const int piece = w.refused[k] / SUB;
-        bool first = true;                                       // once per piece
-        for (int j = 0; j < k; j++) first &= w.refused[j] / SUB != piece;
-        if (!first) continue;
+    plain_sums(tid, WALK_THREADS);
+    // pieces that hold a refused token are summed again without it
+    for (int k0 = 0; !PROBS && k0 < w.n_refused; k0 += WARPS) {
+      const int k = k0 + warp, piece = k < w.n_refused ? w.refused[k] / SUB : -1;
+      double s = 0.0;
+      if (piece >= 0) {
         float z[16];
         const T *z0 = logits_of(cur);
         load_piece(z0, piece * SUB, width, aligned4(z0), z);
-        double s = 0.0;
 #pragma unroll
         for (int e = 0; e < 16; e++) {
           const int x = piece * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
-          bool out = false;
+          bool out = x >= width;
           for (int j = 0; j < w.n_refused; j++) out |= w.refused[j] == x;
-          if (!out && x < width) s += weight(z[e], zm, inv_t, tab);
+          if (!out) s += weight(z[e], tab);
         }
         s = warp_sum64(s);
-        if (lane == 0) s_sub[piece] = s;
       }
-      __syncthreads();
+      __syncthreads();                                           // (after the plain sums)
+      if (piece >= 0 && lane == 0) s_sub[piece] = s;             // (twice in the same piece: the same sum)
     }
+    __syncthreads();
   }
   if (warp == 0) {
     int drop = PROBS ? 0 : w.n_refused;
-    double total = 0.0;
-    for (int k = lane; k < a.n_sub; k += 32) total += s_sub[k];
-    total = warp_sum64(total);
+    auto sum_all = [&]() {
+      double t = 0.0;
+      for (int k = lane; k < a.n_sub; k += 32) t += s_sub[k];
+      return warp_sum64(t);
+    };
+    double total = sum_all();
     if (!none && !(total > 0.0) && drop) {                       // nothing is left: from p itself
       drop = 0;
-      const float zm = w.zmax[cur];
-      const float *sm = a.sub_max + (size_t)(row0 + cur) * a.n_sub;
-      const double *su = a.sub_sum + (size_t)(row0 + cur) * a.n_sub;
-      for (int k = lane; k < a.n_sub; k += 32) {
-        const float km = sm[k];
-        s_sub[k] = km > -INFINITY ? su[k] * weight(km, zm, inv_t, tab) : 0.0;
-      }
-      total = w.z[cur];
+      plain_sums(lane, 32);
       __syncwarp();
+      total = sum_all();
     }
     int token = 0;                                               // a row without a number gives its lowest id
     if (!none || residual) {
       const double target = (double)w.u[0] * total;
       double before = 0.0;
-      const int piece = search_sums(a.n_sub, target, [&](int k) { return s_sub[k]; }, &before);
+      const int piece = search_sums(a.n_sub, target, s_sub, &before);
       if (piece >= 0) {
-        float z[16], q[16];
         const T *z0 = logits_of(cur);
-        load_piece(z0, piece * SUB, width, aligned4(z0), z);
-        if (residual) load_piece(probs_of(cur), piece * SUB, width, aligned4(probs_of(cur)), q);
+        const double inv_z = residual && !none ? 1.0 / w.z[cur] : 1.0;
         double wt[16];
 #pragma unroll
         for (int e = 0; e < 16; e++) {
-          const int x = piece * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
-          double v = none ? (x == 0 ? 1.0 : 0.0) : weight(z[e], w.zmax[cur], inv_t, tab);
-          if (residual) v = fmax((none ? v : v * (1.0 / w.z[cur])) - w.beta * (double)fmaxf(q[e], 0.f), 0.0);
+          const int x = piece * SUB + 16 * lane + e;
+          double v = 0.0;
+          if (x < width) {
+            v = none ? (x == 0 ? 1.0 : 0.0) : weight(to_f(z0[x]), tab) * inv_z;
+            if (residual) v = fmax(v - w.beta * (double)fmaxf(probs_of(cur)[x], 0.f), 0.0);
+          }
           for (int j = 0; j < drop; j++)
             if (w.refused[j] == x) v = 0.0;
-          wt[e] = x < width ? v : 0.0;
+          wt[e] = v;
         }
-        token = search_piece(before, target, piece * SUB, wt);
-        if (token < 0) token = 0;
+        token = max(search_ids(before, target, piece * SUB, wt), 0);
       }
     }
     int *om = a.out_m + seq, *ot = a.out_tok + (size_t)seq * a.out_width, *op = a.out_path + (size_t)seq * a.out_width;
     for (int k = lane; k < a.out_width; k += 32) {
       op[k] = k <= m ? w.path[k] : -1;
-      ot[k] = k < m ? w.tok[w.path[k + 1]] : k == m ? a.lo + token : -1;
+      ot[k] = a.lo + (k < m ? w.tok[w.path[k + 1]] : token);
+      if (k > m) ot[k] = -1;
     }
     if (lane == 0) *om = m;
   }
@@ -510,7 +565,11 @@ inline cudaError_t enqueue_t(const Args &a, const EpArgs &ea, int n_seq, int tot
   if (e != cudaSuccess) return e;
   cfg.blockDim = dim3(WALK_THREADS);
   cfg.dynamicSmemBytes = a.n_sub * sizeof(double);
-  cfg.gridDim = dim3(a.probs ? n_seq * CLUSTER : n_seq);
+  // a pass over the vocabulary is shared by as many CTAs as leave every tree's an SM of their own
+  int ranks = 1;
+  while (a.probs && ranks < CLUSTER && 2 * ranks * n_seq <= 148 && 2 * ranks <= a.n_sub) ranks *= 2;
+  cfg.gridDim = dim3(ranks * n_seq);
+  at[1].val.clusterDim.x = ranks;
   if (a.probs) cfg.numAttrs = 2;
   return a.probs ? cudaLaunchKernelEx(&cfg, walk_kernel<T, true, CTX>, a, ea) : cudaLaunchKernelEx(&cfg, walk_kernel<T, false, CTX>, a, ea);
 }

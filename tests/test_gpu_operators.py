@@ -181,6 +181,20 @@ def test_linear_epilogue(kind, act, T, N, K):
     _b().linear_status()
 
 
+@pytest.mark.parametrize("kind", [BF, I8])
+def test_linear_of_more_tiles_than_fit_at_once(kind):
+    """Persistent CTAs take several tiles each, over both accumulator buffers."""
+    g = _gen(12)
+    T, N, K = 1500, 5001, 272
+    x, w, xs, ws = operands(g, T, N, K, kind)
+    bias, r = _randn(g, N), _randn(g, T, N)
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    y = _b().linear(cu(x), cu(w), cu(bias), "silu", cu(r), cu(xs), cu(ws), dtype=F32)
+    want, mag = ref.linear(x, w, bias, "silu", r, xs, ws)
+    check_linear(y, want, mag, K, kind, F32, "silu", bias, r)
+    _b().linear_status()
+
+
 def test_linear_strided_operands_and_odd_k():
     g = _gen(8)
     T, N, K = 19, 70, 333
