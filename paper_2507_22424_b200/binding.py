@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -53,26 +54,11 @@ class Stats(C.Structure):
                 ("ms_loop", C.c_float), ("device_loop", C.c_int)]
 
 
-class NormArgs(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("rows", "d", "type", "code_type")] + \
-               [("x", C.c_void_p), ("ldx", C.c_longlong), ("residual", C.c_void_p), ("ld_residual", C.c_longlong),
-                ("gain", C.c_void_p), ("sum", C.c_void_p), ("ld_sum", C.c_longlong),
-                ("codes", C.c_void_p), ("ld_codes", C.c_longlong), ("scale", C.c_void_p), ("eps", C.c_float)]
-
-
-class LinearArgs(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("T", "N", "K", "type", "out_type", "act")] + \
-               [("X", C.c_void_p), ("ldx", C.c_longlong), ("x_scale", C.c_void_p),
-                ("W", C.c_void_p), ("ldw", C.c_longlong), ("w_scale", C.c_void_p), ("bias", C.c_void_p),
-                ("residual", C.c_void_p), ("ld_residual", C.c_longlong), ("Y", C.c_void_p), ("ldy", C.c_longlong),
-                ("status", C.c_void_p)]
-
-
-class VerifyArgs(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("n_seq", "rows", "vocab", "lo", "hi", "logits_type")] + \
-               [("logits", C.c_void_p), ("ld_logits", C.c_longlong), ("draft_probs", C.c_void_p),
-                ("ld_draft", C.c_longlong), ("temperature", C.c_float)] + \
-               [(n, C.c_void_p) for n in ("tokens", "parent", "n_rows", "u", "accept_len", "path", "tokens_out")]
+# Argument blocks of the stand-alone operators (specvla_norm_args, specvla_linear_args, specvla_verify_args), packed
+# in native alignment: a third of the time that filling a ctypes structure takes.
+NORM_ARGS = struct.Struct("@4i PqPqP PqPq P f")
+LINEAR_ARGS = struct.Struct("@6i PqP PqP P Pq Pq P")
+VERIFY_ARGS = struct.Struct("@6i PqPq f 7P")
 
 
 EXPORTS = {
@@ -112,13 +98,13 @@ EXPORTS = {
     "specvla_verify_tree_sampled": (C.c_int, [C.c_void_p, C.c_int, C.POINTER(C.c_int), C.POINTER(Tree), C.c_float,
                                               C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int), C.c_void_p,
                                               C.c_void_p]),
-    "specvla_rmsnorm_q8": (C.c_int, [C.POINTER(NormArgs), C.c_void_p]),
+    "specvla_rmsnorm_q8": (C.c_int, [C.c_void_p, C.c_void_p]),
     "specvla_quantize_rows": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_longlong, C.c_void_p, C.c_int,
                                         C.c_longlong, C.c_void_p, C.c_void_p]),
-    "specvla_linear": (C.c_int, [C.POINTER(LinearArgs), C.c_void_p]),
+    "specvla_linear": (C.c_int, [C.c_void_p, C.c_void_p]),
     "specvla_linear_fault_test": (C.c_int, [C.c_longlong, C.c_int]),
     "specvla_verify_sampled_scratch_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int]),
-    "specvla_verify_sampled": (C.c_int, [C.POINTER(VerifyArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "specvla_verify_sampled": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "specvla_profile": (C.c_int, [C.c_void_p, C.c_int]),
     "specvla_profile_read": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_longlong),
                                        C.POINTER(C.c_double)]),
@@ -295,7 +281,7 @@ class SpecVLA:
                 rows += len(t["tokens"])
             if rows != u.numel():
                 raise ValueError(f"{u.numel()} random numbers for {rows} rows")
-        _check_cuda(u)
+        _device(u)
         if u.dtype != torch.float32 or not u.is_contiguous():
             raise ValueError("u must be a contiguous float32 tensor")
         logits = torch.empty(u.numel(), self.model.vocab, dtype=torch.float32, device="cuda")
@@ -451,42 +437,42 @@ class GemmRunner:
 # ---------------------------------------------------------------------- stand-alone operators
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, torch.float8_e4m3fn: 4}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
-_CODES = (torch.int8, torch.float8_e4m3fn)
+_FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
+_CODES = frozenset((torch.int8, torch.float8_e4m3fn))
 _status_words = {}
 
 
-def _check_cuda(*tensors):
-    """The library works on the current device: tensors elsewhere are refused."""
-    dev = torch.cuda.current_device()
+def _device(*tensors):
+    """The current device, on which the library works: tensors elsewhere are refused."""
+    dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"tensor on {t.device}, current device is cuda:{dev}")
+    return dev
 
 
-def _rows(t, name, shape=None, dtypes=None):
-    """A matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError(f"{name} must be a matrix with contiguous rows")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
-    if dtypes is not None and t.dtype not in dtypes:
+def _rows(t, name, rows, cols, dtypes):
+    """Row distance of a matrix [rows, cols] with contiguous rows."""
+    if t.dtype not in dtypes:
         raise ValueError(f"{name} has type {t.dtype}")
-    return t
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    return ld if ld > cols else cols
 
 
 def _vector(t, name, n):
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous()):
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 vector of {n}")
-    return t
+    return t.data_ptr()
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _ld(t):
-    return 0 if t is None else max(t.stride(0), t.shape[1])
+def _matrix(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    return t.shape
 
 
 def _run(rc):
@@ -498,53 +484,53 @@ def rmsnorm_q8(x, gain=None, residual=None, eps=1e-6, dtype=torch.int8, out_sum=
     """specvla_rmsnorm_q8 over the rows of x [rows, d] (f32 / bf16 / f16): codes (int8 or float8_e4m3fn), scale
     [rows], and the sum x + residual in x's type (None without a residual). out_sum: where the sum goes; x and
     residual themselves are allowed."""
-    _rows(x, "x", dtypes=_FLOATS)
-    rows, d = x.shape
+    rows, d = _matrix(x, "x")
+    ldx = _rows(x, "x", rows, d, _FLOATS)
     if dtype not in _CODES:
         raise ValueError(f"codes of type {dtype}")
-    _vector(gain, "gain", d)
-    total = None
+    gain_p = 0 if gain is None else _vector(gain, "gain", d)
+    total, ldr, lds, res_p, sum_p = None, 0, 0, 0, 0
     if residual is not None:
-        _rows(residual, "residual", x.shape, (x.dtype,))
-        total = torch.empty_like(x, memory_format=torch.contiguous_format) if out_sum is None else \
-            _rows(out_sum, "out_sum", x.shape, (x.dtype,))
+        same = (x.dtype,)
+        ldr, res_p = _rows(residual, "residual", rows, d, same), residual.data_ptr()
+        total = x.new_empty((rows, d)) if out_sum is None else out_sum
+        lds, sum_p = _rows(total, "out_sum", rows, d, same), total.data_ptr()
     elif out_sum is not None:
         raise ValueError("out_sum without a residual")
-    _check_cuda(x, gain, residual, total)
-    codes = torch.empty(rows, d, dtype=dtype, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    dev = _device(x, gain, residual, total)
+    codes = x.new_empty((rows, d), dtype=dtype)
+    scale = x.new_empty(rows, dtype=torch.float32)
     if rows and d:
-        _run(lib.specvla_rmsnorm_q8(C.byref(NormArgs(
-            rows, d, TYPES[x.dtype], TYPES[dtype], x.data_ptr(), _ld(x), _ptr(residual), _ld(residual), _ptr(gain),
-            _ptr(total), _ld(total), codes.data_ptr(), d, scale.data_ptr(), eps)), _stream()))
+        _run(lib.specvla_rmsnorm_q8(
+            NORM_ARGS.pack(rows, d, TYPES[x.dtype], TYPES[dtype], x.data_ptr(), ldx, res_p, ldr, gain_p, sum_p, lds,
+                           codes.data_ptr(), d, scale.data_ptr(), eps), torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale, total
 
 
 def quantize_rows(x, dtype=torch.int8):
     """specvla_quantize_rows over the rows of x [rows, d]: codes and scale [rows]."""
-    _rows(x, "x", dtypes=_FLOATS)
+    rows, d = _matrix(x, "x")
+    ldx = _rows(x, "x", rows, d, _FLOATS)
     if dtype not in _CODES:
         raise ValueError(f"codes of type {dtype}")
-    _check_cuda(x)
-    rows, d = x.shape
-    codes = torch.empty(rows, d, dtype=dtype, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    dev = _device(x)
+    codes = x.new_empty((rows, d), dtype=dtype)
+    scale = x.new_empty(rows, dtype=torch.float32)
     if rows and d:
-        _run(lib.specvla_quantize_rows(C.c_void_p(x.data_ptr()), TYPES[x.dtype], rows, d, _ld(x),
-                                       C.c_void_p(codes.data_ptr()), TYPES[dtype], d, C.c_void_p(scale.data_ptr()),
-                                       _stream()))
+        _run(lib.specvla_quantize_rows(x.data_ptr(), TYPES[x.dtype], rows, d, ldx, codes.data_ptr(), TYPES[dtype], d,
+                                       scale.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale
 
 
-def _status_word():
+def _status_word(dev):
     """The status word of this module's linear() calls on the current device (linear_status reads it)."""
-    dev = torch.cuda.current_device()
-    if dev not in _status_words:
+    word = _status_words.get(dev)
+    if word is None:
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("the first linear() on a device must not be inside a stream capture")
-        _status_words[dev] = torch.zeros(1, dtype=torch.int32, device="cuda")
+        word = _status_words[dev] = torch.zeros(1, dtype=torch.int32, device="cuda")
         torch.cuda.synchronize()
-    return _status_words[dev]
+    return word
 
 
 def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=None, dtype=None, out=None):
@@ -552,41 +538,62 @@ def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=Non
     float8_e4m3fn), scales f32 [T] and [N] with the 8-bit ones, bias f32 [N]; dtype: of the result and the residual
     (default: x's, bf16 for 8-bit operands). out: where the result goes, the residual itself is allowed.
     Asynchronous: linear_status() reports a device-side wait that gave up."""
-    _rows(x, "x", dtypes=(torch.bfloat16, torch.float16) + _CODES)
-    T, K = x.shape
-    _rows(w, "w", (w.shape[0], K), (x.dtype,))
-    N = w.shape[0]
+    T, K = _matrix(x, "x")
+    N = _matrix(w, "w")[0]
+    kind = x.dtype
+    codes = kind in _CODES
+    if not codes and kind != torch.bfloat16 and kind != torch.float16:
+        raise ValueError(f"x has type {kind}")
+    same = (kind,)
+    ldx, ldw = _rows(x, "x", T, K, same), _rows(w, "w", N, K, same)
     if dtype is None:
-        dtype = out.dtype if out is not None else torch.bfloat16 if x.dtype in _CODES else x.dtype
+        dtype = out.dtype if out is not None else torch.bfloat16 if codes else kind
     if dtype not in _FLOATS:
         raise ValueError(f"result of type {dtype}")
     if act not in ACTS:
         raise ValueError(f"activation {act!r}: one of {', '.join(ACTS)}")
-    if (x_scale is not None or w_scale is not None) and x.dtype not in _CODES:
+    if (x_scale is not None or w_scale is not None) and not codes:
         raise ValueError("scales belong to 8-bit operands")
-    _vector(bias, "bias", N), _vector(x_scale, "x_scale", T), _vector(w_scale, "w_scale", N)
+    bias_p = 0 if bias is None else _vector(bias, "bias", N)
+    xs_p = 0 if x_scale is None else _vector(x_scale, "x_scale", T)
+    ws_p = 0 if w_scale is None else _vector(w_scale, "w_scale", N)
+    ldr, res_p = 0, 0
     if residual is not None:
-        _rows(residual, "residual", (T, N), (dtype,))
-    y = torch.empty(T, N, dtype=dtype, device=x.device) if out is None else _rows(out, "out", (T, N), (dtype,))
-    _check_cuda(x, w, bias, residual, x_scale, w_scale, y)
+        ldr, res_p = _rows(residual, "residual", T, N, (dtype,)), residual.data_ptr()
+    y = x.new_empty((T, N), dtype=dtype) if out is None else out
+    ldy = _rows(y, "out", T, N, (dtype,))
+    dev = _device(x, w, bias, residual, x_scale, w_scale, y)
     if T and N:
         if not K:
             raise ValueError("K is 0")
-        _run(lib.specvla_linear(C.byref(LinearArgs(
-            T, N, K, TYPES[x.dtype], TYPES[dtype], ACTS[act], x.data_ptr(), _ld(x), _ptr(x_scale), w.data_ptr(), _ld(w),
-            _ptr(w_scale), _ptr(bias), _ptr(residual), _ld(residual), y.data_ptr(), _ld(y),
-            _status_word().data_ptr())), _stream()))
+        _run(lib.specvla_linear(
+            LINEAR_ARGS.pack(T, N, K, TYPES[kind], TYPES[dtype], ACTS[act], x.data_ptr(), ldx, xs_p, w.data_ptr(), ldw, ws_p,
+                             bias_p, res_p, ldr, y.data_ptr(), ldy, _status_word(dev).data_ptr()),
+            torch._C._cuda_getCurrentRawStream(dev)))
     return y
 
 
 def linear_status():
     """Synchronises the current stream; raises SpecVLAError(-6) if a linear() call on this device gave up since the
     last time (its result is undefined), and clears the status."""
-    word = _status_word()
+    word = _status_word(_device())
     rc = lib.specvla_gemm_status(C.c_void_p(word.data_ptr()), _stream())
     if rc != 0:
         word.zero_()
     _run(rc)
+
+
+def _row_distance(t, name, n, rows, vocab):
+    s = t.stride()
+    if t.shape != (n, rows, vocab) or s[2] != 1 or (n > 1 and s[0] != rows * s[1]) or (n * rows > 1 and s[1] < vocab):
+        raise ValueError(f"{name} must be {(n, rows, vocab)} with rows at one distance")
+    return s[1] if s[1] > vocab else vocab
+
+
+def _whole(t, name, dtype, shape):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {shape}")
+    return t.data_ptr()
 
 
 def verify_sampled(logits, tokens, parent, u, n_rows=None, temperature=1.0, draft_probs=None, lo=0, hi=None):
@@ -597,34 +604,24 @@ def verify_sampled(logits, tokens, parent, u, n_rows=None, temperature=1.0, draf
         raise ValueError("logits must be [trees, rows, vocab] of f32, bf16 or f16")
     n, rows, vocab = logits.shape
     hi = vocab if hi is None else hi
-
-    def flat(t, name):
-        if tuple(t.shape) != (n, rows, vocab) or t.stride(2) != 1 or (n > 1 and t.stride(0) != rows * t.stride(1)) or \
-                (n * rows > 1 and t.stride(1) < vocab):
-            raise ValueError(f"{name} must be [{n}, {rows}, {vocab}] with rows at one distance")
-        return max(t.stride(1), vocab)
-
-    ld = flat(logits, "logits")
-    ldp = 0
+    ld, ldp, probs_p = _row_distance(logits, "logits", n, rows, vocab), 0, 0
     if draft_probs is not None:
-        if draft_probs.dtype != torch.float32:
-            raise ValueError("draft_probs must be float32")
-        ldp = flat(draft_probs, "draft_probs")
-    for t, name, dt, shape in ((tokens, "tokens", torch.int32, (n, rows)), (parent, "parent", torch.int32, (n, rows)),
-                               (u, "u", torch.float32, (n, rows)), (n_rows, "n_rows", torch.int32, (n,))):
-        if t is not None and (t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous {dt} {shape}")
-    _check_cuda(logits, tokens, parent, u, n_rows, draft_probs)
-    m = torch.empty(n, dtype=torch.int32, device=logits.device)
-    path = torch.empty(n, rows, dtype=torch.int32, device=logits.device)
-    out = torch.empty(n, rows, dtype=torch.int32, device=logits.device)
+        if draft_probs.dtype != torch.float32 or draft_probs.dim() != 3:
+            raise ValueError("draft_probs must be float32 [trees, rows, vocab]")
+        ldp, probs_p = _row_distance(draft_probs, "draft_probs", n, rows, vocab), draft_probs.data_ptr()
+    shape = (n, rows)
+    tok_p, par_p = _whole(tokens, "tokens", torch.int32, shape), _whole(parent, "parent", torch.int32, shape)
+    u_p = _whole(u, "u", torch.float32, shape)
+    rows_p = 0 if n_rows is None else _whole(n_rows, "n_rows", torch.int32, (n,))
+    dev = _device(logits, tokens, parent, u, n_rows, draft_probs)
+    m, path, out = tokens.new_empty(n), tokens.new_empty(shape), tokens.new_empty(shape)
     if n:
         nb = lib.specvla_verify_sampled_scratch_bytes(n, rows, lo, hi)
         if nb == 0:
             raise SpecVLAError(-1, f"({n} trees of {rows} rows over ids [{lo}, {hi}))")
-        scratch = torch.empty(nb, dtype=torch.uint8, device=logits.device)
-        _run(lib.specvla_verify_sampled(C.byref(VerifyArgs(
-            n, rows, vocab, lo, hi, TYPES[logits.dtype], logits.data_ptr(), ld, _ptr(draft_probs), ldp, temperature,
-            tokens.data_ptr(), parent.data_ptr(), _ptr(n_rows), u.data_ptr(), m.data_ptr(), path.data_ptr(),
-            out.data_ptr())), C.c_void_p(scratch.data_ptr()), nb, _stream()))
+        scratch = tokens.new_empty(nb, dtype=torch.uint8)
+        _run(lib.specvla_verify_sampled(
+            VERIFY_ARGS.pack(n, rows, vocab, lo, hi, TYPES[logits.dtype], logits.data_ptr(), ld, probs_p, ldp, temperature,
+                             tok_p, par_p, rows_p, u_p, m.data_ptr(), path.data_ptr(), out.data_ptr()),
+            scratch.data_ptr(), nb, torch._C._cuda_getCurrentRawStream(dev)))
     return m, path, out

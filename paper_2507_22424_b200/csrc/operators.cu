@@ -128,12 +128,12 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
     double cost = 1e30;
     const int cmin = (T + linear::MAX_TN - 1) / linear::MAX_TN;
-    for (int c = cmin; c <= 4 * cmin + 4 && c <= T; c++) {
+    for (int c = cmin; c <= 8 * cmin + 4 && c <= T; c++) {
       const int tn = ((T + c - 1) / c + 31) / 32 * 32;
-      if (tn > linear::MAX_TN || tn < 64) continue;
+      if (tn > linear::MAX_TN || tn < 32) continue;
       const int chunks = (T + tn - 1) / tn;
       const long long waves = ((long long)tiles * chunks + pairs - 1) / pairs;
-      const double k = waves * (double)(KB * (tn + 32) + 1000);
+      const double k = waves * (double)((double)KB * (256 + tn) + 8000 + 24 * tn);
       if (k < cost) {
         cost = k;
         best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2};
@@ -220,7 +220,7 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   a.T = l->T, a.N = l->N;
   a.KB = (int)((bytes + linear::KBYTES - 1) / linear::KBYTES);
   a.act = l->act;
-  a.pairs = aligned(l->Y, 2 * eo) && (l->T == 1 || l->ldy % 2 == 0) &&
+  a.pairs = l->N % 2 == 0 && aligned(l->Y, 2 * eo) && (l->T == 1 || l->ldy % 2 == 0) &&
             (!l->residual || (aligned(l->residual, 2 * eo) && (l->T == 1 || l->ld_residual % 2 == 0)));
   a.x_scale = l->x_scale, a.w_scale = l->w_scale, a.bias = l->bias;
   a.res = l->residual, a.ldr = l->ld_residual;
