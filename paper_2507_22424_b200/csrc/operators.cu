@@ -57,9 +57,25 @@ int norm_launch(const norm_q8::Args &a, int rows, void *stream) {
                    (!a.s || (aligned(a.s, 16) && a.lds % V == 0)) && (!a.gain || aligned(a.gain, 16)) &&
                    aligned(a.q, V) && a.ldq % V == 0;
   // as many vectors a thread as it keeps; with fewer rows than SMs one, so that all loads are in flight at once
-  const long long n = (a.d + (vec ? V : 1) - 1) / (vec ? V : 1);
-  const long long per = rows <= 148 ? 1 : norm_q8::cached(vec ? V : 1);
+  const int step = vec ? V : 1, keep = 16 / step;
+  const long long n = (a.d + step - 1) / step, per = rows <= 148 ? 1 : keep;
   const int threads = (int)std::min(1024ll, std::max(64ll, (n + 32 * per - 1) / (32 * per) * 32));
+  // many rows: CTAs that copy ahead, 1024 threads on an SM
+  if (vec && rows > 148 * 4) {
+    auto go = [&](auto kernel, int nt) {
+      const size_t smem = (size_t)(a.r ? 2 : 1) * nt * 32 * sizeof(T);
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
+        return (int)SPECVLA_ERR_CUDA;
+      }
+      const int ctas = (int)std::min<size_t>(1024 / nt, 200 * 1024 / smem);
+      return launch(kernel, dim3(std::min(rows, 148 * ctas)), dim3(nt), smem, 1, stream, a);
+    };
+    if (a.d <= 64 * 32) return go(norm_q8::norm_q8_rows_kernel<T, CODE, 64>, 64);
+    if (a.d <= 128 * 32) return go(norm_q8::norm_q8_rows_kernel<T, CODE, 128>, 128);
+    if (a.d <= 256 * 32) return go(norm_q8::norm_q8_rows_kernel<T, CODE, 256>, 256);
+    if (a.d <= 512 * 32) return go(norm_q8::norm_q8_rows_kernel<T, CODE, 512>, 512);
+  }
   return launch(vec ? norm_q8::norm_q8_kernel<T, CODE, V> : norm_q8::norm_q8_kernel<T, CODE, 1>, dim3(rows), dim3(threads), 0, 1,
                 stream, a);
 }
@@ -179,8 +195,8 @@ int specvla_rmsnorm_q8(const specvla_norm_args *n, void *stream) {
   const size_t e = bytes_of(n->type);
   if (!aligned(n->x, e) || !aligned(n->residual, e) || !aligned(n->sum, e) || !aligned(n->gain, 4) || !aligned(n->scale, 4))
     return SPECVLA_ERR_INVALID_ARG;
-  const norm_q8::Args a = {n->x, n->residual, n->gain, n->sum, static_cast<unsigned char *>(n->codes), n->scale, n->d,
-                           n->ldx, n->ld_residual, n->ld_sum, n->ld_codes, n->eps, 1};
+  const norm_q8::Args a = {n->x, n->residual, n->gain, n->sum, static_cast<unsigned char *>(n->codes), n->scale, n->rows,
+                           n->d, n->ldx, n->ld_residual, n->ld_sum, n->ld_codes, n->eps, 1};
   return norm_entry(a, n->rows, n->type, n->code_type, stream);
 }
 
@@ -189,7 +205,7 @@ int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ld
   if (!X || !codes || !scale || rows < 1 || d < 1 || ldx < d || ld_codes < d || !is_float(type) || !is_code(code_type) ||
       !aligned(X, bytes_of(type)) || !aligned(scale, 4))
     return SPECVLA_ERR_INVALID_ARG;
-  const norm_q8::Args a = {X, nullptr, nullptr, nullptr, static_cast<unsigned char *>(codes), scale, d, ldx, 0, 0, ld_codes, 0.f, 0};
+  const norm_q8::Args a = {X, nullptr, nullptr, nullptr, static_cast<unsigned char *>(codes), scale, rows, d, ldx, 0, 0, ld_codes, 0.f, 0};
   return norm_entry(a, rows, type, code_type, stream);
 }
 
@@ -274,6 +290,7 @@ int specvla_verify_sampled(const specvla_verify_args *v, void *scratch, size_t s
   a.lo = v->lo, a.hi = v->hi;
   a.n_sub = sampled::pieces_of(v->hi - v->lo);
   a.temperature = v->temperature;
+  a.factor = sampled::exp_factor(v->temperature);
   a.u = v->u;
   a.tokens = v->tokens, a.parent = v->parent, a.n_rows = v->n_rows;
   a.rows = v->rows;

@@ -19,6 +19,7 @@
 // shared memory, and the drawn token takes a search over the sums of 512 ids and one warp's scan.
 #pragma once
 #include <cooperative_groups.h>
+#include <algorithm>
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -30,6 +31,7 @@ constexpr int STATS_THREADS = 256;
 constexpr int WALK_THREADS = 512;
 constexpr int CLUSTER = 8;                // largest
 constexpr int MAX_IDS = 1 << 20;          // ids that may take part
+inline double exp_factor(float temperature) { return 92.332482616893657 / (double)temperature; }
 inline int pieces_of(int ids) { return (ids + SUB - 1) / SUB; }
 
 struct Args {
@@ -39,7 +41,9 @@ struct Args {
   long long ld_probs;
   int lo, hi;
   int n_sub;                              // pieces of SUB ids
+  int per_cta;                            // ... that a CTA of the first launch takes
   float temperature;
+  double factor;                          // 64 / (ln 2 temperature)
   const float *u;                         // [rows], in the order of the logits' rows
   // trees, as arrays ...
   const int *tokens, *parent, *n_rows;    // [n_seq][rows]; n_rows [n_seq] or NULL
@@ -82,16 +86,16 @@ struct ExpTable { double t[64]; };
 __device__ __forceinline__ void fill(ExpTable &tab) {
   if (threadIdx.x < 64) tab.t[threadIdx.x] = EXP2_64[threadIdx.x];
 }
-__device__ __forceinline__ double exp_factor(float temperature) { return 92.332482616893657 / (double)temperature; }
 // Weights of one row: exp((z - zmax) / temperature) = 2^(y / 64) with y = (z - zmax) 64 / (ln 2 temperature) = n + r,
 // n whole, |r| <= 1/2: a table entry, a power of two and a polynomial of degree 4 in r (the first term left out is
-// below 4e-14). Ten 64-bit operations with the sum. zmax has 1, an infinite one too; a NaN, and what lies below e^-700, 0.
+// below 4e-14). Ten 64-bit operations with the sum. zmax has 1, an infinite one too; a NaN, and what lies below e^-300, 0.
 struct RowExp {
   float zmax, low;
   double k;
   __device__ __forceinline__ RowExp(float zm, float temperature, double k_)
-      : zmax(zm), low(zm - 700.f * temperature), k(k_) {}
-  __device__ __forceinline__ double operator()(float z, const ExpTable &tab) const {
+      : zmax(zm), low(fmaxf(zm - 300.f * temperature, -3.4028235e38f)), k(k_) {}
+  // zmax finite, low <= z <= zmax (low is rounded: twice the distance at most)
+  __device__ __forceinline__ double inner(float z, const ExpTable &tab) const {
     constexpr double MAGIC = 6755399441055744.0;               // 1.5 * 2^52
     const double d = (double)z - (double)zmax;
     const double m = fma(d, k, MAGIC);
@@ -102,8 +106,15 @@ struct RowExp {
     p = fma(p, r, 0.010830424696249145);
     p = fma(p, r, 1.0);
     const double t = tab.t[n & 63];
-    p *= __hiloint2double(__double2hiint(t) + ((n >> 6) << 20), __double2loint(t));
-    return z == zmax ? 1.0 : z > low ? p : 0.0;
+    return p * __hiloint2double(__double2hiint(t) + ((n >> 6) << 20), __double2loint(t));
+  }
+  __device__ __forceinline__ double operator()(float z, const ExpTable &tab) const {
+    return z == zmax ? 1.0 : finite(z, tab);
+  }
+  // the same where zmax is finite
+  __device__ __forceinline__ double finite(float z, const ExpTable &tab) const {
+    const double p = inner(z, tab);
+    return z >= low ? p : 0.0;
   }
 };
 
@@ -113,21 +124,23 @@ __device__ __forceinline__ double warp_sum64(double v) {
   return v;
 }
 
-// 16 ids of a lane: ids 128 j + 4 lane + e of the piece that starts at `first`; -inf past `end`.
-template <typename T> __device__ __forceinline__ void load_piece(const T *row, int first, int end, bool vec, float (&z)[16]) {
-  const int lane = threadIdx.x & 31;
+// 16 ids of a lane: ids 128 j + 4 lane + e of the piece that starts at `first`, or (RUN) 16 lane + 4 j + e; -inf past
+// `end`. Loads first, selections after: behind a branch each load would wait for the one before it.
+template <bool RUN, typename T> __device__ __forceinline__ void load_piece(const T *row, int first, int end, bool vec, float (&z)[16]) {
+  const int lane = threadIdx.x & 31, base = first + (RUN ? 16 : 4) * lane, step = RUN ? 4 : 128;
+  if (vec && first + SUB <= end) {
+    struct alignas(4 * sizeof(T)) Four { T e[4]; };
+    Four v[4];
 #pragma unroll
-  for (int j = 0; j < 4; j++) {
-    const int i = first + 128 * j + 4 * lane;
-    if (vec && i + 4 <= end) {
-      struct alignas(4 * sizeof(T)) Four { T e[4]; };
-      const Four v = *reinterpret_cast<const Four *>(row + i);
+    for (int j = 0; j < 4; j++) v[j] = *reinterpret_cast<const Four *>(row + base + step * j);
 #pragma unroll
-      for (int e = 0; e < 4; e++) z[4 * j + e] = to_f(v.e[e]);
-    } else {
+    for (int k = 0; k < 16; k++) z[k] = to_f(v[k >> 2].e[k & 3]);
+  } else {
+    T v[16];
 #pragma unroll
-      for (int e = 0; e < 4; e++) z[4 * j + e] = i + e < end ? to_f(row[i + e]) : -INFINITY;
-    }
+    for (int k = 0; k < 16; k++) v[k] = row[min(base + step * (k >> 2) + (k & 3), end - 1)];
+#pragma unroll
+    for (int k = 0; k < 16; k++) z[k] = base + step * (k >> 2) + (k & 3) < end ? to_f(v[k]) : -INFINITY;
   }
 }
 // Whether four elements at a multiple of four ids after lo are aligned.
@@ -135,39 +148,49 @@ template <typename T> __device__ __forceinline__ bool aligned4(const T *p) {
   return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
 }
 
-// CTX: row numbers of a context's call (no rows are left out).
+// CTX: row numbers of a context's call (no rows are left out). A CTA takes a.per_cta pieces of one row, its warps in turn;
+// a warp asks for its next piece before it sums the present one.
 template <typename T, bool CTX>
-static __global__ void __launch_bounds__(STATS_THREADS) stats_kernel(const Args a, int total_rows) {
+static __global__ void __launch_bounds__(STATS_THREADS, 5) stats_kernel(const Args a) {
   __shared__ ExpTable tab;
   fill(tab);
   pdl_wait();
   pdl_launch();
-  __syncthreads();
-  const int lane = threadIdx.x & 31;
-  const long long piece = (long long)blockIdx.x * (STATS_THREADS / 32) + (threadIdx.x >> 5);
-  if (piece >= (long long)total_rows * a.n_sub) return;
-  const int row = (int)(piece / a.n_sub), sub = (int)(piece - (long long)row * a.n_sub);
+  const int row = blockIdx.x, lane = threadIdx.x & 31;
   if (!CTX && a.n_rows) {
     const int seq = row / a.rows;
     if (row - seq * a.rows >= max(a.n_rows[seq], 1)) return;
   }
+  const int end = min(a.n_sub, ((int)blockIdx.y + 1) * a.per_cta), width = a.hi - a.lo;
+  int sub = (int)blockIdx.y * a.per_cta + (threadIdx.x >> 5);
   const T *z0 = static_cast<const T *>(a.logits) + row * a.ld + a.lo;
-  float z[16];
-  load_piece(z0, sub * SUB, a.hi - a.lo, aligned4(z0), z);
-  float m = -INFINITY;
+  const bool vec = aligned4(z0);
+  float z[16], next[16];
+  if (sub < end) load_piece<false>(z0, sub * SUB, width, vec, next);
+  __syncthreads();
+  for (; sub < end; sub += STATS_THREADS / 32) {
+    float m = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 16; k++) m = fmaxf(m, z[k]);             // (a NaN loses)
-  m = warp_max(m);
-  const RowExp weight(m, a.temperature, exp_factor(a.temperature));
-  double s = 0.0;
-  if (m > -INFINITY) {
+    for (int k = 0; k < 16; k++) {
+      z[k] = next[k];
+      m = fmaxf(m, z[k]);                                      // (a NaN loses)
+    }
+    if (sub + STATS_THREADS / 32 < end) load_piece<false>(z0, (sub + STATS_THREADS / 32) * SUB, width, vec, next);
+    m = warp_max(m);
+    const RowExp weight(m, a.temperature, a.factor);
+    double s = 0.0;
+    if (m < INFINITY && m > -INFINITY) {
 #pragma unroll
-    for (int k = 0; k < 16; k++) s += weight(z[k], tab);
-  }
-  s = warp_sum64(s);
-  if (lane == 0) {
-    a.sub_max[(size_t)row * a.n_sub + sub] = m;
-    a.sub_sum[(size_t)row * a.n_sub + sub] = s;
+      for (int k = 0; k < 16; k++) s += weight.finite(z[k], tab);
+    } else if (m > 0.f) {                                      // infinite logits share the row
+#pragma unroll
+      for (int k = 0; k < 16; k++) s += z[k] == m ? 1.0 : 0.0;
+    }
+    s = warp_sum64(s);
+    if (lane == 0) {
+      a.sub_max[(size_t)row * a.n_sub + sub] = m;
+      a.sub_sum[(size_t)row * a.n_sub + sub] = s;
+    }
   }
 }
 
@@ -176,8 +199,9 @@ struct Walk {
   double z[SV_MAX_TREE];                  // its sum of weights; 0: nothing to draw from, the lowest id has all
   double w[SV_MAX_TREE];                  // weight of the row's token in its parent's row (PROBS: over its sum)
   float q[SV_MAX_TREE], u[SV_MAX_TREE];
-  int tok[SV_MAX_TREE], parent[SV_MAX_TREE];
+  int tok[SV_MAX_TREE];
   int inner[SV_MAX_TREE];                 // the row has children
+  alignas(16) int parent[SV_MAX_TREE];    // -1 past the last row
   int yes[SV_MAX_TREE];                   // no PROBS: the row is accepted if the walk comes to it
   int again[SV_MAX_TREE];                 // no PROBS: an elder sibling has the same token
   int path[SV_MAX_TREE];
@@ -251,7 +275,7 @@ __device__ __forceinline__ int search_ids(double before, double target, int firs
 
 // Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends.
 template <typename T, bool PROBS, bool CTX>
-static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args a, const EpArgs ea) {
+static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kernel(const Args a, const EpArgs ea) {
   namespace cg = cooperative_groups;
   __shared__ ExpTable tab;
   __shared__ Walk w;
@@ -260,14 +284,13 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
   if (PROBS) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (that every CTA has started)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int WARPS = WALK_THREADS / 32;
-  if (tid < SV_MAX_TREE) w.inner[tid] = 0;
+  if (tid < SV_MAX_TREE) w.inner[tid] = 0, w.parent[tid] = -1;
   int rank = 0, ranks = 1;
   if (PROBS) {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   }
   const int seq = (int)blockIdx.x / ranks;
-  const double factor = exp_factor(a.temperature);
   pdl_wait();
   pdl_launch();
   const DevTree *tr = CTX ? a.trees + ea.eps[seq] : nullptr;
@@ -288,6 +311,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
   __syncthreads();
   int my_parent = -1, my_x = -1;
   float my_z = 0.f, my_q = 0.f;
+  uint32_t elder[4];
   if (tid < n) {
     my_x = (int)((unsigned)(CTX ? tr->tok[tid] : a.tokens[row0 + tid]) - (unsigned)a.lo);
     my_parent = CTX ? tr->parent[tid] : a.parent[row0 + tid];
@@ -308,12 +332,21 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
     if (!w.inner[i]) continue;
     const float *sm = maxima_of(i);
     const double *su = sums_of(i);
-    const float m = row_max(sm);
-    const RowExp weight(m, a.temperature, factor);
+    // (the first 64 pieces' values are asked for together)
+    const int k0 = min(lane, a.n_sub - 1), k1 = min(lane + 32, a.n_sub - 1);
+    const float m0 = sm[k0], m1 = sm[k1];
+    const double s0 = su[k0], s1 = su[k1];
+    float m = fmaxf(m0, m1);
+    for (int k = lane + 64; k < a.n_sub; k += 32) m = fmaxf(m, sm[k]);
+    m = warp_max(m);
+    const RowExp weight(m, a.temperature, a.factor);
     double z = 0.0;
-    if (m > -INFINITY)
-      for (int k = lane; k < a.n_sub; k += 32)
+    if (m > -INFINITY) {
+      if (lane < a.n_sub && m0 > -INFINITY) z = s0 * weight(m0, tab);
+      if (lane + 32 < a.n_sub && m1 > -INFINITY) z += s1 * weight(m1, tab);
+      for (int k = lane + 64; k < a.n_sub; k += 32)
         if (sm[k] > -INFINITY) z += su[k] * weight(sm[k], tab);
+    }
     z = warp_sum64(z);
     if (lane == 0) w.zmax[i] = m, w.z[i] = z;
   }
@@ -324,7 +357,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
   __syncthreads();
   // weight of id x of a row with children, and the sum of its row
   auto weight_of = [&](int i, float z, int x) {
-    return w.z[i] > 0.0 ? RowExp(w.zmax[i], a.temperature, factor)(z, tab) : x == 0 ? 1.0 : 0.0;
+    return w.z[i] > 0.0 ? RowExp(w.zmax[i], a.temperature, a.factor)(z, tab) : x == 0 ? 1.0 : 0.0;
   };
   auto sum_of = [&](int i) { return w.z[i] > 0.0 ? w.z[i] : 1.0; };
   if (tid < n) {
@@ -332,8 +365,23 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
     w.w[tid] = PROBS ? (inside ? v / sum_of(my_parent) : 0.0) : v;
     w.q[tid] = my_q;
     if (!PROBS) {
+      // the row's elder siblings, a bit each
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        elder[k] = 0;
+        if (32 * k < tid && my_parent >= 0) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            const int4 p = *reinterpret_cast<const int4 *>(&w.parent[32 * k + j]);
+            elder[k] |= (uint32_t)((p.x == my_parent) | (p.y == my_parent) << 1 | (p.z == my_parent) << 2 | (p.w == my_parent) << 3) << j;
+          }
+          if (32 * k + 31 >= tid) elder[k] &= (1u << (tid & 31)) - 1;
+        }
+      }
       bool again = false;
-      for (int j = 1; j < tid; j++) again |= w.parent[j] == my_parent && w.tok[j] == my_x;
+#pragma unroll
+      for (int k = 0; k < 4; k++)
+        for (uint32_t left = elder[k]; left; left &= left - 1) again |= w.tok[32 * k + __ffs(left) - 1] == my_x;
       w.again[tid] = again;
     }
   }
@@ -344,8 +392,12 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
       bool yes = false;
       if (inside && !w.again[tid]) {
         double S = sum_of(my_parent);
-        for (int j = 1; j < tid; j++)
-          if (w.parent[j] == my_parent && !w.again[j]) S -= w.w[j];
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+          for (uint32_t left = elder[k]; left; left &= left - 1) {
+            const int j = 32 * k + __ffs(left) - 1;
+            if (!w.again[j]) S -= w.w[j];
+          }
         yes = w.w[tid] > 0.0 && (double)w.u[tid] * S < w.w[tid];
       }
       w.yes[tid] = yes;
@@ -413,15 +465,15 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
       const int cur = w.cur;
       const bool none = !(w.z[cur] > 0.0);
       const double beta = w.beta, inv_z = 1.0 / sum_of(cur);
-      const RowExp weight(w.zmax[cur], a.temperature, factor);
+      const RowExp weight(w.zmax[cur], a.temperature, a.factor);
       const T *z0 = logits_of(cur);
       const float *q0 = probs_of(cur);
       const bool vz = aligned4(z0), vq = aligned4(q0);
       double mine = 0.0;
       for (int k = warp * ranks + rank; k < a.n_sub; k += WARPS * ranks) {
         float z[16], q[16];
-        load_piece(z0, k * SUB, width, vz, z);
-        load_piece(q0, k * SUB, width, vq, q);
+        load_piece<false>(z0, k * SUB, width, vz, z);
+        load_piece<false>(q0, k * SUB, width, vq, q);
         double s = 0.0;
 #pragma unroll
         for (int e = 0; e < 16; e++) {
@@ -467,7 +519,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
   const float *sm = maxima_of(cur);
   const double *su = sums_of(cur);
   const float zm = w.inner[cur] ? w.zmax[cur] : row_max(sm);
-  const RowExp weight(zm, a.temperature, factor);
+  const RowExp weight(zm, a.temperature, a.factor);
   const bool none = !(zm > -INFINITY);
   auto plain_sums = [&](int first, int step) {
     for (int k = first; k < a.n_sub; k += step) s_sub[k] = sm[k] > -INFINITY ? su[k] * weight(sm[k], tab) : 0.0;
@@ -481,13 +533,16 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
       if (piece >= 0) {
         float z[16];
         const T *z0 = logits_of(cur);
-        load_piece(z0, piece * SUB, width, aligned4(z0), z);
+        load_piece<false>(z0, piece * SUB, width, aligned4(z0), z);
+        uint32_t out = 0;                                        // this lane's refused ones
+        for (int j = 0; j < w.n_refused; j++) {
+          const int at = w.refused[j] - piece * SUB;
+          if (at >= 0 && at < SUB && (at >> 2 & 31) == lane) out |= 1u << (at >> 7 << 2 | (at & 3));
+        }
 #pragma unroll
         for (int e = 0; e < 16; e++) {
-          const int x = piece * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
-          bool out = x >= width;
-          for (int j = 0; j < w.n_refused; j++) out |= w.refused[j] == x;
-          if (!out) s += weight(z[e], tab);
+          const double v = weight(z[e], tab);                    // (past the last id: -inf)
+          s += out >> e & 1 ? 0.0 : v;
         }
         s = warp_sum64(s);
       }
@@ -518,18 +573,21 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
       if (piece >= 0) {
         const T *z0 = logits_of(cur);
         const double inv_z = residual && !none ? 1.0 / w.z[cur] : 1.0;
+        float z[16], q[16];
+        load_piece<true>(z0, piece * SUB, width, aligned4(z0), z);
+        if (residual) load_piece<true>(probs_of(cur), piece * SUB, width, aligned4(probs_of(cur)), q);
         double wt[16];
 #pragma unroll
         for (int e = 0; e < 16; e++) {
           const int x = piece * SUB + 16 * lane + e;
-          double v = 0.0;
-          if (x < width) {
-            v = none ? (x == 0 ? 1.0 : 0.0) : weight(to_f(z0[x]), tab) * inv_z;
-            if (residual) v = fmax(v - w.beta * (double)fmaxf(probs_of(cur)[x], 0.f), 0.0);
-          }
-          for (int j = 0; j < drop; j++)
-            if (w.refused[j] == x) v = 0.0;
-          wt[e] = v;
+          double v = none ? (x == 0 ? 1.0 : 0.0) : weight(z[e], tab) * inv_z;
+          if (residual) v = fmax(v - w.beta * (double)fmaxf(q[e], 0.f), 0.0);
+          wt[e] = x < width ? v : 0.0;
+        }
+        for (int j = 0; j < drop; j++) {
+          const int at = w.refused[j] - (piece * SUB + 16 * lane);
+#pragma unroll
+          for (int e = 0; e < 16; e++) wt[e] = at == e ? 0.0 : wt[e];
         }
         token = max(search_ids(before, target, piece * SUB, wt), 0);
       }
@@ -546,7 +604,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, 2) walk_kernel(const Args
 
 // Both launches; type: of the logits (f32, bf16, f16). A context's call has its rows in ea and its trees in a.trees.
 template <typename T, bool CTX>
-inline cudaError_t enqueue_t(const Args &a, const EpArgs &ea, int n_seq, int total_rows, cudaStream_t st) {
+inline cudaError_t enqueue_t(Args a, const EpArgs &ea, int n_seq, int total_rows, cudaStream_t st) {
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -558,16 +616,20 @@ inline cudaError_t enqueue_t(const Args &a, const EpArgs &ea, int n_seq, int tot
   cfg.stream = st;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  const long long pieces = (long long)total_rows * a.n_sub;
-  cfg.gridDim = dim3((unsigned)((pieces + STATS_THREADS / 32 - 1) / (STATS_THREADS / 32)));
+  // one piece a warp while there are few, up to three (816 rows of 32064 ids with their walk: 55 us, with one 58, with eight
+  // 61; 51 rows: 15, with two 16, with eight 22)
+  constexpr int WARPS = STATS_THREADS / 32;
+  const long long all = (long long)total_rows * a.n_sub, room = 148ll * 128;
+  a.per_cta = WARPS * (int)std::min(3ll, std::max(1ll, (all + room - 1) / room));
+  cfg.gridDim = dim3(total_rows, (a.n_sub + a.per_cta - 1) / a.per_cta);
   cfg.blockDim = dim3(STATS_THREADS);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a, total_rows);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a);
   if (e != cudaSuccess) return e;
   cfg.blockDim = dim3(WALK_THREADS);
   cfg.dynamicSmemBytes = a.n_sub * sizeof(double);
-  // a pass over the vocabulary is shared by as many CTAs as leave every tree's an SM of their own
+  // a pass over the vocabulary is shared by as many CTAs as run at once, two on an SM
   int ranks = 1;
-  while (a.probs && ranks < CLUSTER && 2 * ranks * n_seq <= 148 && 2 * ranks <= a.n_sub) ranks *= 2;
+  while (a.probs && ranks < CLUSTER && 2 * ranks * n_seq <= 2 * 148 && 2 * ranks <= a.n_sub) ranks *= 2;
   cfg.gridDim = dim3(ranks * n_seq);
   at[1].val.clusterDim.x = ranks;
   if (a.probs) cfg.numAttrs = 2;

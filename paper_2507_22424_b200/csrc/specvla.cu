@@ -1307,6 +1307,7 @@ static int verify_device_trees(specvla_ctx *ctx, const EpArgs &ea, int R, int r,
     argmax_range(ctx, &a.lo, &a.hi);
     a.n_sub = sampled::pieces_of(a.hi - a.lo);
     a.temperature = temperature;
+    a.factor = sampled::exp_factor(temperature);
     a.u = u;
     a.trees = ctx->trees;
     // (the greedy argmax is done with its candidates: 16 bytes per 128 ids and row, where 12 per 512 are needed)
