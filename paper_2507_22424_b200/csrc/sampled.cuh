@@ -42,6 +42,7 @@ struct Args {
   int lo, hi;
   int n_sub;                              // pieces of SUB ids
   int per_cta;                            // ... that a CTA of the first launch takes
+  int kept;                               // ... whose probabilities a warp of the second keeps between passes over a row
   float temperature;
   double factor;                          // 64 / (ln 2 temperature)
   const float *u;                         // [rows], in the order of the logits' rows
@@ -101,7 +102,7 @@ struct RowExp {
     const double m = fma(d, k, MAGIC);
     const int n = __double2loint(m);
     const double r = fma(d, k, MAGIC - m);
-    double p = fma(r, 5.7328516886404019e-10, 2.1173137155464776e-07);
+    double p = fma(r, 5.7328516886404019e-10, 2.1173137155464776e-07);                               // (ln 2 / 64)^j / j!
     p = fma(p, r, 5.86490495505617e-05);
     p = fma(p, r, 0.010830424696249145);
     p = fma(p, r, 1.0);
@@ -111,11 +112,12 @@ struct RowExp {
   __device__ __forceinline__ double operator()(float z, const ExpTable &tab) const {
     return z == zmax ? 1.0 : finite(z, tab);
   }
-  // the same where zmax is finite
   __device__ __forceinline__ double finite(float z, const ExpTable &tab) const {
     const double p = inner(z, tab);
     return z >= low ? p : 0.0;
   }
+  // the same for a sum that zmax is part of (zmax finite, low < zmax): what counts as 0 gives e^-300 at most
+  __device__ __forceinline__ double summand(float z, const ExpTable &tab) const { return inner(fmaxf(z, low), tab); }
 };
 
 __device__ __forceinline__ double warp_sum64(double v) {
@@ -179,12 +181,12 @@ static __global__ void __launch_bounds__(STATS_THREADS, 5) stats_kernel(const Ar
     m = warp_max(m);
     const RowExp weight(m, a.temperature, a.factor);
     double s = 0.0;
-    if (m < INFINITY && m > -INFINITY) {
+    if (m < INFINITY && weight.low < m) {
 #pragma unroll
-      for (int k = 0; k < 16; k++) s += weight.finite(z[k], tab);
-    } else if (m > 0.f) {                                      // infinite logits share the row
+      for (int k = 0; k < 16; k++) s += weight.summand(z[k], tab);
+    } else if (m > -INFINITY) {                                // infinite logits share the row, or the temperature is next to 0
 #pragma unroll
-      for (int k = 0; k < 16; k++) s += z[k] == m ? 1.0 : 0.0;
+      for (int k = 0; k < 16; k++) s += weight(z[k], tab);
     }
     s = warp_sum64(s);
     if (lane == 0) {
@@ -208,8 +210,7 @@ struct Walk {
   int refused[SV_MAX_TREE];               // tokens refused at the row where the walk ends, each once
   int n_refused, cur, next, m, want;      // want: the walk waits for a pass over the vocabulary
   double beta, S;
-  double part[2][CLUSTER];                // sums of the cluster's CTAs, by turns
-  double warp_part[WALK_THREADS / 32];
+  double part[2][CLUSTER * WALK_THREADS / 32];   // sums of the cluster's warps, by turns
 };
 
 // The piece at `target` of n sums (whole warp), and the cumulative sum before it; the last piece that has any weight
@@ -273,7 +274,8 @@ __device__ __forceinline__ int search_ids(double before, double target, int firs
   return some ? __shfl_sync(0xffffffffu, any, 31 - __clz(some)) : -1;
 }
 
-// Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends.
+// Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends; PROBS: then p and q of the
+// first a.kept pieces of every warp.
 template <typename T, bool PROBS, bool CTX>
 static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kernel(const Args a, const EpArgs ea) {
   namespace cg = cooperative_groups;
@@ -429,8 +431,12 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
             beta = 0.0, S = 1.0;
             if (lane == 0) w.path[m] = c;
           } else {
+            // the sum of what is left: the row's first (1), with another child to come (3), a later one (2)
+            unsigned others = 0;
+            for (int i1 = i0; i1 < n && !others; i1 += 32)
+              others = __ballot_sync(0xffffffffu, i1 + lane < n && w.parent[i1 + lane] == cur);
+            want = beta > 0.0 ? 2 : others ? 3 : 1;
             beta += S;
-            want = 1;                                            // the sum of what is left
           }
         }
         if (lane == 0) w.cur = cur, w.m = m, w.next = i0, w.beta = beta, w.S = S, w.want = want;
@@ -461,46 +467,57 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
     __syncthreads();
     if (!PROBS || !w.want) break;
     if constexpr (PROBS) {
-      // S = sum of max(p - beta q, 0): pieces go round the cluster's warps; their sums stay for the search
+      // S = sum of max(p - beta q, 0): pieces go round the cluster's warps; their sums stay for the search, and p and q in
+      // shared memory for the row's next pass
       const int cur = w.cur;
-      const bool none = !(w.z[cur] > 0.0);
+      const bool none = !(w.z[cur] > 0.0), first = w.want != 2, keep = w.want == 3;
       const double beta = w.beta, inv_z = 1.0 / sum_of(cur);
       const RowExp weight(w.zmax[cur], a.temperature, a.factor);
       const T *z0 = logits_of(cur);
       const float *q0 = probs_of(cur);
       const bool vz = aligned4(z0), vq = aligned4(q0);
       double mine = 0.0;
-      for (int k = warp * ranks + rank; k < a.n_sub; k += WARPS * ranks) {
-        float z[16], q[16];
-        load_piece<false>(z0, k * SUB, width, vz, z);
-        load_piece<false>(q0, k * SUB, width, vq, q);
-        double s = 0.0;
+      for (int k = warp * ranks + rank, n = 0; k < a.n_sub; k += WARPS * ranks, n++) {
+        double p[16], s = 0.0;
+        float q[16];
+        double *kp = s_sub + a.n_sub + ((size_t)n * WARPS + warp) * 768 + lane;   // 16 x 32 of p, then of q
+        if (first || n >= a.kept) {
+          float z[16];
+          load_piece<false>(z0, k * SUB, width, vz, z);
+          load_piece<false>(q0, k * SUB, width, vq, q);
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const int x = k * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
-          const double p = none ? (x == 0 ? 1.0 : 0.0) : weight(z[e], tab) * inv_z;
-          if (x < width) s += fmax(p - beta * (double)fmaxf(q[e], 0.f), 0.0);
+          for (int e = 0; e < 16; e++) {
+            const int x = k * SUB + 128 * (e >> 2) + 4 * lane + (e & 3);
+            p[e] = none ? (x == 0 ? 1.0 : 0.0) : weight(z[e], tab) * inv_z;      // (past the last id: -inf)
+            q[e] = fmaxf(q[e], 0.f);
+          }
+          if (keep && n < a.kept) {
+            float *kq = reinterpret_cast<float *>(kp + 512 - lane) + lane;
+#pragma unroll
+            for (int e = 0; e < 16; e++) kp[32 * e] = p[e], kq[32 * e] = q[e];
+          }
+        } else {
+          const float *kq = reinterpret_cast<const float *>(kp + 512 - lane) + lane;
+#pragma unroll
+          for (int e = 0; e < 16; e++) p[e] = kp[32 * e], q[e] = kq[32 * e];
         }
+#pragma unroll
+        for (int e = 0; e < 16; e++) s += fmax(fma(-beta, (double)q[e], p[e]), 0.0);
         s = warp_sum64(s);
         if (lane == 0) s_sub[k] = s;
         mine += s;
       }
-      if (lane == 0) w.warp_part[warp] = mine;
-      __syncthreads();
-      if (tid < ranks) {
-        double s = 0.0;
-        for (int k = 0; k < WARPS; k++) s += w.warp_part[k];
-        *cg::this_cluster().map_shared_rank(&w.part[turn][rank], tid) = s;
-      }
+      if (lane < ranks) *cg::this_cluster().map_shared_rank(&w.part[turn][rank * WARPS + warp], lane) = mine;
       if (ranks > 1) cg::this_cluster().sync();
       else __syncthreads();
-      if (tid == 0) {
+      if (warp == 0) {
         double s = 0.0;
-        for (int k = 0; k < ranks; k++) s += w.part[turn][k];
-        w.S = s;
+        for (int k = lane; k < ranks * WARPS; k += 32) s += w.part[turn][k];
+        s = warp_sum64(s);
+        if (lane == 0) w.S = s;
+        __syncwarp();
       }
       turn ^= 1;
-      __syncthreads();
     }
   }
 
@@ -623,16 +640,22 @@ inline cudaError_t enqueue_t(Args a, const EpArgs &ea, int n_seq, int total_rows
   a.per_cta = WARPS * (int)std::min(3ll, std::max(1ll, (all + room - 1) / room));
   cfg.gridDim = dim3(total_rows, (a.n_sub + a.per_cta - 1) / a.per_cta);
   cfg.blockDim = dim3(STATS_THREADS);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a);
-  if (e != cudaSuccess) return e;
+  cudaError_t err = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a);
+  if (err != cudaSuccess) return err;
   cfg.blockDim = dim3(WALK_THREADS);
   cfg.dynamicSmemBytes = a.n_sub * sizeof(double);
   // a pass over the vocabulary is shared by as many CTAs as run at once, two on an SM
   int ranks = 1;
   while (a.probs && ranks < CLUSTER && 2 * ranks * n_seq <= 2 * 148 && 2 * ranks <= a.n_sub) ranks *= 2;
+  constexpr size_t KEPT = WALK_THREADS / 32 * 768 * sizeof(double);   // bytes of one piece per warp
+  a.kept = a.probs && a.n_sub <= WALK_THREADS / 32 * ranks ? 1 : 0;
+  cfg.dynamicSmemBytes += a.kept * KEPT;
   cfg.gridDim = dim3(ranks * n_seq);
   at[1].val.clusterDim.x = ranks;
   if (a.probs) cfg.numAttrs = 2;
+  if (a.kept && (err = cudaFuncSetAttribute(walk_kernel<T, true, CTX>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            (int)(MAX_IDS / SUB * sizeof(double) + KEPT))) != cudaSuccess)
+    return err;
   return a.probs ? cudaLaunchKernelEx(&cfg, walk_kernel<T, true, CTX>, a, ea) : cudaLaunchKernelEx(&cfg, walk_kernel<T, false, CTX>, a, ea);
 }
 template <bool CTX>
