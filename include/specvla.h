@@ -240,7 +240,7 @@ int specvla_verify_tree(specvla_ctx *ctx, int n_ep, const int *episodes,
  * specvla_verify_sampled without draft probabilities (the draft tree holds the draft model's best tokens, it
  * is not drawn from it): whatever the tree, the emitted tokens have the target's distribution. Relaxed
  * acceptance does not apply.
- *   temperature  > 0
+ *   temperature  > 0, at most 1e30
  *   u            device f32 [total rows], rows in call order: numbers in [0, 1); the root's draws the last token
  *   logits       device f32 [total rows, vocab], written and read */
 int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees,
@@ -436,7 +436,7 @@ typedef struct {
   int logits_type;                /* SPECVLA_F32, BF16 or F16 */
   const void *logits; long long ld_logits;
   const float *draft_probs; long long ld_draft;         /* [n_seq * rows][vocab] or NULL */
-  float temperature;              /* > 0 */
+  float temperature;              /* > 0, at most 1e30 */
   const int *tokens, *parent;     /* [n_seq][rows]; row 0 is the root */
   const int *n_rows;              /* [n_seq] or NULL: all rows */
   const float *u;                 /* [n_seq][rows] in [0, 1): u of row i >= 1 decides it, u of row 0 draws the last token */

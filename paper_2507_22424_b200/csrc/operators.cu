@@ -140,7 +140,9 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   for (int s = 2; fit && s <= linear::MAX_S; s++)
     if ((long long)fit->clusters[s] >= (long long)p.tiles * p.chunks && KB / s >= 4) p.S = s;
   best = p;
-  if (T > 128 && fit && fit->clusters[2] > 0) {
+  // pairs of CTAs for more than 128 rows, and where the slices would take more than one round (27 x 32064 x 4096 in int8: 25.6 us
+  // as 251 slices of 128 columns on 148 SMs, 23.7 as 126 tiles of 256 on 74 pairs; 11008 columns, one round: the same)
+  if (fit && fit->clusters[2] > 0 && (T > 128 || (long long)p.tiles * p.chunks > fit->clusters[1])) {
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
     double cost = 1e30;
     const int cmin = (T + linear::MAX_TN - 1) / linear::MAX_TN;
@@ -277,7 +279,7 @@ int specvla_verify_sampled(const specvla_verify_args *v, void *scratch, size_t s
     return SPECVLA_ERR_INVALID_ARG;
   const size_t need = specvla_verify_sampled_scratch_bytes(v->n_seq, v->rows, v->lo, v->hi);
   if (need == 0 || v->hi > v->vocab || v->ld_logits < v->vocab || (v->draft_probs && v->ld_draft < v->vocab) || !is_float(v->logits_type) ||
-      !(v->temperature > 0.f) || v->temperature > 3e38f)
+      !(v->temperature > 0.f) || v->temperature > sampled::MAX_TEMPERATURE)
     return SPECVLA_ERR_INVALID_ARG;
   if (!aligned(scratch, 8) || !aligned(v->logits, bytes_of(v->logits_type)) || !aligned(v->draft_probs, 4) || !aligned(v->tokens, 4) ||
       !aligned(v->parent, 4) || !aligned(v->n_rows, 4) || !aligned(v->u, 4) || !aligned(v->accept_len, 4) || !aligned(v->path, 4) ||

@@ -31,6 +31,7 @@ constexpr int STATS_THREADS = 256;
 constexpr int WALK_THREADS = 512;
 constexpr int CLUSTER = 8;                // largest
 constexpr int MAX_IDS = 1 << 20;          // ids that may take part
+constexpr float MAX_TEMPERATURE = 1e30f;   // (300 temperatures below any logit is still a number)
 inline double exp_factor(float temperature) { return 92.332482616893657 / (double)temperature; }
 inline int pieces_of(int ids) { return (ids + SUB - 1) / SUB; }
 

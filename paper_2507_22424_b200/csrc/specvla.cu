@@ -1422,7 +1422,7 @@ int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes,
                                 float temperature, const float *u, int *accept_len_out, int *tokens_out,
                                 float *logits, void *stream) {
   TRY(check_episodes(ctx, n_ep, episodes));
-  if (!(temperature > 0.f) || temperature > 3e38f || !u || !accept_len_out || !tokens_out || !logits) return SPECVLA_ERR_INVALID_ARG;
+  if (!(temperature > 0.f) || temperature > sampled::MAX_TEMPERATURE || !u || !accept_len_out || !tokens_out || !logits) return SPECVLA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   EpArgs ea{};
   int R = 0;
