@@ -480,10 +480,17 @@ def _run(rc):
         raise SpecVLAError(rc)
 
 
+def _codes_like(x, rows, d, dtype):
+    """Codes of [rows, d], rows 16 bytes apart or a multiple of it, as linear() takes them; and that distance."""
+    ld = (d + 15) & -16
+    codes = x.new_empty((rows, ld), dtype=dtype)
+    return (codes if ld == d else codes[:, :d]), ld
+
+
 def rmsnorm_q8(x, gain=None, residual=None, eps=1e-6, dtype=torch.int8, out_sum=None):
-    """specvla_rmsnorm_q8 over the rows of x [rows, d] (f32 / bf16 / f16): codes (int8 or float8_e4m3fn), scale
-    [rows], and the sum x + residual in x's type (None without a residual). out_sum: where the sum goes; x and
-    residual themselves are allowed."""
+    """specvla_rmsnorm_q8 over the rows of x [rows, d] (f32 / bf16 / f16): codes (int8 or float8_e4m3fn; rows start on 16
+    bytes, as linear() takes them), scale [rows], and the sum x + residual in x's type (None without a residual).
+    out_sum: where the sum goes; x and residual themselves are allowed."""
     rows, d = _matrix(x, "x")
     ldx = _rows(x, "x", rows, d, _FLOATS)
     if dtype not in _CODES:
@@ -498,12 +505,12 @@ def rmsnorm_q8(x, gain=None, residual=None, eps=1e-6, dtype=torch.int8, out_sum=
     elif out_sum is not None:
         raise ValueError("out_sum without a residual")
     dev = _device(x, gain, residual, total)
-    codes = x.new_empty((rows, d), dtype=dtype)
+    codes, ldq = _codes_like(x, rows, d, dtype)
     scale = x.new_empty(rows, dtype=torch.float32)
     if rows and d:
         _run(lib.specvla_rmsnorm_q8(
             NORM_ARGS.pack(rows, d, TYPES[x.dtype], TYPES[dtype], x.data_ptr(), ldx, res_p, ldr, gain_p, sum_p, lds,
-                           codes.data_ptr(), d, scale.data_ptr(), eps), torch._C._cuda_getCurrentRawStream(dev)))
+                           codes.data_ptr(), ldq, scale.data_ptr(), eps), torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale, total
 
 
@@ -514,10 +521,10 @@ def quantize_rows(x, dtype=torch.int8):
     if dtype not in _CODES:
         raise ValueError(f"codes of type {dtype}")
     dev = _device(x)
-    codes = x.new_empty((rows, d), dtype=dtype)
+    codes, ldq = _codes_like(x, rows, d, dtype)
     scale = x.new_empty(rows, dtype=torch.float32)
     if rows and d:
-        _run(lib.specvla_quantize_rows(x.data_ptr(), TYPES[x.dtype], rows, d, ldx, codes.data_ptr(), TYPES[dtype], d,
+        _run(lib.specvla_quantize_rows(x.data_ptr(), TYPES[x.dtype], rows, d, ldx, codes.data_ptr(), TYPES[dtype], ldq,
                                        scale.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scale
 
