@@ -126,7 +126,7 @@ const Fit *cluster_fit() {
 // How a call is cut. pair: tiles of 256 columns by pairs of CTAs; else tiles of 128 columns by clusters of S CTAs.
 struct Plan {
   bool pair;
-  int tn, tiles, chunks, S, grid;
+  int tn, tiles, chunks, S, grid, raster;
 };
 Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   Plan best = {};
@@ -158,6 +158,9 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
       }
     }
   }
+  // chunks side by side: 32 MB of X stay in L2 while W streams past (4764 x 22016 x 4096 in e4m3: 290 MB read from memory with
+  // eight, 116 with all nineteen)
+  best.raster = (int)std::min<long long>(best.chunks, std::max<long long>(4, (32ll << 20) / ((long long)best.tn * KB * linear::KBYTES)));
   return best;
 }
 
@@ -172,7 +175,7 @@ int linear_launch(const CUtensorMap &mw, const CUtensorMap &mx, const linear::Ar
   }
   if (p.pair)
     return launch(pair, dim3(p.grid), dim3(linear::PAIR_THREADS), linear::SMEM, 2, stream, mw, mx, a,
-                  linear::PairTiles{p.tiles, p.chunks, 8});
+                  linear::PairTiles{p.tiles, p.chunks, p.raster});
   return launch(slice, dim3(p.tiles * p.S, p.chunks), dim3(linear::THREADS), linear::SMEM, p.S, stream, mw, mx, a, p.S);
 }
 template <int KIND>
