@@ -154,7 +154,7 @@ template <typename T> __device__ __forceinline__ bool aligned4(const T *p) {
 // CTX: row numbers of a context's call (no rows are left out). A CTA takes a.per_cta pieces of one row, its warps in turn;
 // a warp asks for its next piece before it sums the present one.
 template <typename T, bool CTX>
-static __global__ void __launch_bounds__(STATS_THREADS, 5) stats_kernel(const Args a) {
+static __global__ void __launch_bounds__(STATS_THREADS, 6) stats_kernel(const Args a) {
   __shared__ ExpTable tab;
   fill(tab);
   pdl_wait();
@@ -168,17 +168,12 @@ static __global__ void __launch_bounds__(STATS_THREADS, 5) stats_kernel(const Ar
   int sub = (int)blockIdx.y * a.per_cta + (threadIdx.x >> 5);
   const T *z0 = static_cast<const T *>(a.logits) + row * a.ld + a.lo;
   const bool vec = aligned4(z0);
-  float z[16], next[16];
-  if (sub < end) load_piece<false>(z0, sub * SUB, width, vec, next);
   __syncthreads();
   for (; sub < end; sub += STATS_THREADS / 32) {
-    float m = -INFINITY;
+    float z[16], m = -INFINITY;
+    load_piece<false>(z0, sub * SUB, width, vec, z);
 #pragma unroll
-    for (int k = 0; k < 16; k++) {
-      z[k] = next[k];
-      m = fmaxf(m, z[k]);                                      // (a NaN loses)
-    }
-    if (sub + STATS_THREADS / 32 < end) load_piece<false>(z0, (sub + STATS_THREADS / 32) * SUB, width, vec, next);
+    for (int k = 0; k < 16; k++) m = fmaxf(m, z[k]);           // (a NaN loses)
     m = warp_max(m);
     const RowExp weight(m, a.temperature, a.factor);
     double s = 0.0;
