@@ -241,11 +241,12 @@ int specvla_verify_tree(specvla_ctx *ctx, int n_ep, const int *episodes,
  * is not drawn from it): whatever the tree, the emitted tokens have the target's distribution. Relaxed
  * acceptance does not apply.
  *   temperature  > 0, at most 1e30
- *   u            device f32 [total rows], rows in call order: numbers in [0, 1); the root's draws the last token
- *   logits       device f32 [total rows, vocab], written and read */
+ *   u            device f32 [n_rows], rows in call order: numbers in [0, 1); the root's draws the last token
+ *   logits       device f32 [n_rows, vocab], written and read
+ *   n_rows       rows of all trees of the call; SPECVLA_ERR_INVALID_ARG if they have another number */
 int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees,
-                                float temperature, const float *u, int *accept_len_out, int *tokens_out,
-                                float *logits, void *stream);
+                                float temperature, const float *u, float *logits, int n_rows, int *accept_len_out,
+                                int *tokens_out, void *stream);
 
 /* The verification forward alone (Eq. 1 over every tree row): greedy token of M_V after each row
  * of caller-supplied trees, WITHOUT acceptance, compaction or any change of the episodes' state
@@ -376,7 +377,7 @@ typedef struct {
   const void *x;        long long ldx;
   const void *residual; long long ld_residual;   /* may be NULL */
   const float *gain;              /* [d], may be NULL: ones */
-  void *sum;            long long ld_sum;        /* may be NULL; may be x or residual itself (same ld) */
+  void *sum;            long long ld_sum;        /* may be NULL; may be x or residual itself (same ld); x without a residual */
   void *codes;          long long ld_codes;
   float *scale;                   /* [rows] */
   float eps;                      /* >= 0 */
@@ -389,7 +390,7 @@ int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ld
 
 /* Y = act(X_scale[t] W_scale[n] (X W^T)[t][n] + bias[n]) + residual[t][n]
  * X [T, K] and W [N, K] of one type: BF16, F16, I8 or E4M3; scales only for the last two. Products are exact
- * in the accumulator (int8: 32-bit integers, K <= 131071; otherwise fp32); scales, bias, activation and residual are
+ * in the accumulator (int8: 32-bit integers, K <= 131071; otherwise fp32, K <= 2^29); scales, bias, activation and residual are
  * applied in fp32 and the result is rounded once to out_type (F32, BF16, F16). Any T, N, K >= 1; rows of X and W
  * start on 16 bytes (base address and ld); Y and residual on their own element. Y may be the residual itself. Values
  * that are not finite reach what depends on them only.

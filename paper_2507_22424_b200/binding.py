@@ -96,7 +96,7 @@ EXPORTS = {
     "specvla_gemm_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int,
                                      C.c_void_p]),
     "specvla_verify_tree_sampled": (C.c_int, [C.c_void_p, C.c_int, C.POINTER(C.c_int), C.POINTER(Tree), C.c_float,
-                                              C.c_void_p, C.POINTER(C.c_int), C.POINTER(C.c_int), C.c_void_p,
+                                              C.c_void_p, C.c_void_p, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int),
                                               C.c_void_p]),
     "specvla_rmsnorm_q8": (C.c_int, [C.c_void_p, C.c_void_p]),
     "specvla_quantize_rows": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_longlong, C.c_void_p, C.c_int,
@@ -288,8 +288,8 @@ class SpecVLA:
         m = (C.c_int * n)()
         toks = (C.c_int * (n * (MAX_DEPTH + 1)))()
         self._check(lib.specvla_verify_tree_sampled(self.h, n, _ints(episodes), ctrees, float(temperature),
-                                                    C.c_void_p(u.data_ptr()), m, toks, C.c_void_p(logits.data_ptr()),
-                                                    _stream()))
+                                                    C.c_void_p(u.data_ptr()), C.c_void_p(logits.data_ptr()), u.numel(), m,
+                                                    toks, _stream()))
         emitted = [list(toks[i * (MAX_DEPTH + 1): i * (MAX_DEPTH + 1) + m[i] + 1]) for i in range(n)]
         return list(m), emitted, logits
 

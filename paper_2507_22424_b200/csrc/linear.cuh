@@ -84,8 +84,8 @@ __device__ __forceinline__ float fast_gelu(float v) {
   p = fmaf(p, t, 1.421413741f);
   p = fmaf(p, t, -0.284496736f);
   p = fmaf(p, t, 0.254829592f) * t;
-  const float y = 0.5f * v * p * e;
-  return v > 0.f ? v - y : y;
+  const float q = p * e, y = 0.5f * v * q;
+  return v > 0.f ? (q > 0.f ? v - y : v) : y;                  // (infinity stays one)
 }
 template <bool FAST, int M> __device__ __forceinline__ void activate(float (&v)[M], int act) {
   switch (act) {

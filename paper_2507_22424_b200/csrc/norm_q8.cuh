@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) norm_q8_rows_kernel(const Args 
         const Vec<T, V> u = *reinterpret_cast<const Vec<T, V> *>(slot(1, j));
 #pragma unroll
         for (int e = 0; e < V; e++) v.e[e] = from_float<T>(to_float(v.e[e]) + to_float(u.e[e]));
-        if (row.s && in) *reinterpret_cast<Vec<T, V> *>(row.s + i0 + j * STRIDE) = v;
       }
+      if (row.s && in) *reinterpret_cast<Vec<T, V> *>(row.s + i0 + j * STRIDE) = v;
       float g[V];
       if (a.gain) load_gain<V>(a.gain + (full ? i0 + j * STRIDE : min(i0 + j * STRIDE, a.d - V)), g);
 #pragma unroll

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <mutex>
 
@@ -187,13 +188,14 @@ int linear_out(int out_type, const CUtensorMap &mw, const CUtensorMap &mx, const
   }
 }
 
-unsigned long long g_linear_wait_ns = gemm_tc::WAIT_LIMIT_NS;    // of the next call (specvla_linear_fault_test)
-int g_linear_withhold = 0;
+std::atomic<unsigned long long> g_linear_wait_ns{gemm_tc::WAIT_LIMIT_NS};   // of the next call (specvla_linear_fault_test)
+std::atomic<int> g_linear_withhold{0};
+constexpr int MAX_ROW = 1 << 30;         // elements of a row: offsets within one are 32-bit
 
 }  // namespace
 
 int specvla_rmsnorm_q8(const specvla_norm_args *n, void *stream) {
-  if (!n || !n->x || !n->codes || !n->scale || n->rows < 1 || n->d < 1 || !is_float(n->type) || !is_code(n->code_type))
+  if (!n || !n->x || !n->codes || !n->scale || n->rows < 1 || n->d < 1 || n->d > MAX_ROW || !is_float(n->type) || !is_code(n->code_type))
     return SPECVLA_ERR_INVALID_ARG;
   if (n->ldx < n->d || n->ld_codes < n->d || (n->residual && n->ld_residual < n->d) || (n->sum && n->ld_sum < n->d) || !(n->eps >= 0.f))
     return SPECVLA_ERR_INVALID_ARG;
@@ -207,7 +209,7 @@ int specvla_rmsnorm_q8(const specvla_norm_args *n, void *stream) {
 
 int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ldx, void *codes, int code_type,
                           long long ld_codes, float *scale, void *stream) {
-  if (!X || !codes || !scale || rows < 1 || d < 1 || ldx < d || ld_codes < d || !is_float(type) || !is_code(code_type) ||
+  if (!X || !codes || !scale || rows < 1 || d < 1 || d > MAX_ROW || ldx < d || ld_codes < d || !is_float(type) || !is_code(code_type) ||
       !aligned(X, bytes_of(type)) || !aligned(scale, 4))
     return SPECVLA_ERR_INVALID_ARG;
   const norm_q8::Args a = {X, nullptr, nullptr, nullptr, static_cast<unsigned char *>(codes), scale, rows, d, ldx, 0, 0, ld_codes, 0.f, 0};
@@ -227,6 +229,7 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   if (!(codes || l->type == SPECVLA_BF16 || l->type == SPECVLA_F16) || !is_float(l->out_type)) return SPECVLA_ERR_INVALID_ARG;
   if (l->act < SPECVLA_ACT_NONE || l->act > SPECVLA_ACT_SILU) return SPECVLA_ERR_INVALID_ARG;
   if (!codes && (l->x_scale || l->w_scale)) return SPECVLA_ERR_INVALID_ARG;
+  if (l->K > MAX_ROW / 2 || l->N > MAX_ROW || l->T > MAX_ROW) return SPECVLA_ERR_INVALID_ARG;   // (coordinates of copies are 32-bit)
   if (l->type == SPECVLA_I8 && l->K > 131071) return SPECVLA_ERR_INVALID_ARG;       // 2^14 K must fit 31 bits
   const long long e = (long long)bytes_of(l->type), eo = (long long)bytes_of(l->out_type);
   // (a single row has no distance to the next)
@@ -247,10 +250,8 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   a.res = l->residual, a.ldr = l->ld_residual;
   a.y = l->Y, a.ldy = l->ldy;
   a.status = l->status;
-  a.wait_ns = g_linear_wait_ns;
-  a.withhold = g_linear_withhold;
-  g_linear_wait_ns = gemm_tc::WAIT_LIMIT_NS;                     // the test hook holds for one call
-  g_linear_withhold = 0;
+  a.wait_ns = g_linear_wait_ns.exchange(gemm_tc::WAIT_LIMIT_NS);  // the test hook holds for one call
+  a.withhold = g_linear_withhold.exchange(0);
   const int kind = l->type == SPECVLA_I8 ? linear::KIND_I8 : l->type == SPECVLA_E4M3 ? linear::KIND_E4M3 : linear::KIND_16;
   const Plan p = plan_linear(l->T, l->N, a.KB, cluster_fit());
   if (p.chunks > 65535) return SPECVLA_ERR_INVALID_ARG;

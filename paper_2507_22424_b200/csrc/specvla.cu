@@ -1419,14 +1419,18 @@ int specvla_verify_tree(specvla_ctx *ctx, int n_ep, const int *episodes, const s
 }
 
 int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees,
-                                float temperature, const float *u, int *accept_len_out, int *tokens_out,
-                                float *logits, void *stream) {
+                                float temperature, const float *u, float *logits, int n_rows, int *accept_len_out,
+                                int *tokens_out, void *stream) {
   TRY(check_episodes(ctx, n_ep, episodes));
   if (!(temperature > 0.f) || temperature > sampled::MAX_TEMPERATURE || !u || !accept_len_out || !tokens_out || !logits) return SPECVLA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   EpArgs ea{};
   int R = 0;
+  int lo, hi;
+  argmax_range(ctx, &lo, &hi);
+  if (hi - lo > sampled::MAX_IDS) return SPECVLA_ERR_CAPACITY;
   TRY(prepare_trees(ctx, n_ep, episodes, trees, &ea, &R, st));
+  if (n_rows != R) return SPECVLA_ERR_INVALID_ARG;
   TRY(verify_device_trees(ctx, ea, R, 0, logits, st, u, temperature));
   return finish_verify(ctx, ea, accept_len_out, tokens_out, st);
 }

@@ -114,6 +114,39 @@ def test_norm_sum_in_place_and_strided_rows(kind, rows, d):
         assert (wide[:, d:d + 8] == 7).all()
 
 
+@pytest.mark.parametrize("rows", [3, 700])
+def test_norm_sum_without_a_residual_is_x(rows):
+    """Through the C entry point (the binding has no such call): the sum receives x, codes and scale are those of x."""
+    B = _b()
+    x = _randn(_gen(8), rows, 64).half()
+    xc, s = x.cuda(), torch.zeros(rows, 64, dtype=HF, device="cuda")
+    codes, scale = torch.zeros(rows, 64, dtype=I8, device="cuda"), torch.zeros(rows, device="cuda")
+    assert B.lib.specvla_rmsnorm_q8(B.NORM_ARGS.pack(rows, 64, 2, 3, xc.data_ptr(), 64, 0, 0, 0, s.data_ptr(), 64, codes.data_ptr(), 64,
+                                                     scale.data_ptr(), 1e-6), B._stream()) == 0
+    assert torch.equal(s, xc)
+    check_norm(x, None, None, 1e-6, I8, (codes, scale, None))
+
+
+@pytest.mark.parametrize("kind", [F32, BF, HF])
+@pytest.mark.parametrize("d", [64, 1024, 4096, 4104, 8192, 9000, 16384])
+@pytest.mark.parametrize("dtype", [I8, E4])
+def test_norm_of_many_rows(kind, d, dtype):
+    """The kernel that copies ahead: every width of its CTAs, full and partly filled, rows of every sort among ordinary ones."""
+    g = _gen(d)
+    rows = 650
+    x, r = (_randn(g, rows, d) * 2).to(kind), _randn(g, rows, d).to(kind)
+    x[7] = r[7] = 0
+    x[8, 3], x[600, d - 1] = math.nan, math.inf
+    x[9], r[9] = 1e-4, 0
+    gain = 1 + 0.2 * _randn(g, d)
+    gain[: d // 2] = 1                                                # exact products: ties with the middle between two codes
+    check_norm(x, gain, r, 1e-6, dtype, _b().rmsnorm_q8(x.cuda(), gain.cuda(), residual=r.cuda(), dtype=dtype))
+    codes, scale = _b().quantize_rows(x.cuda(), dtype)
+    check_norm(x, None, None, 0.0, dtype, (codes, scale, None), norm=False)
+    xc, rc = x.cuda(), r.cuda()
+    check_norm(x, gain, r, 1e-6, dtype, _b().rmsnorm_q8(xc, gain.cuda(), residual=rc, dtype=dtype, out_sum=xc))
+
+
 @pytest.mark.parametrize("kind", [F32, BF, HF])
 @pytest.mark.parametrize("dtype", [I8, E4])
 def test_quantize_rows(kind, dtype):
@@ -224,6 +257,23 @@ def test_linear_non_finite_values_stay_where_they_belong(T):
     assert torch.equal(~torch.isfinite(y), bad)
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+@pytest.mark.parametrize("T", [3, 200])
+def test_linear_activations_far_out(act, dtype, T):
+    """Infinities, NaN and the tails, by a bias: as the formula gives them, tails within what their fp32 form rounds."""
+    vals = torch.tensor([math.inf, -math.inf, math.nan, 60.0, -60.0, 12.0, -12.0, 6.0, -6.0, 4.0, -4.0, 1e-3, -1e-3, 0.0, -88.0, 100.0, -100.0, 1e30, -1e30])
+    x, w = torch.zeros(T, 16, dtype=HF), torch.zeros(len(vals), 16, dtype=HF)
+    y = _b().linear(x.cuda(), w.cuda(), vals.cuda(), act, dtype=dtype).cpu()
+    want = ref.act(vals.double(), act).to(dtype).double()
+    for row in y.double():
+        fin = torch.isfinite(want)
+        assert torch.equal(torch.isnan(row), torch.isnan(want)) and torch.equal(row[~fin & ~torch.isnan(want)], want[~fin & ~torch.isnan(want)])
+        # 1 + erf and 1 + tanh are off by 2^-23 where they are near 0 (fp32), the 16-bit form of erf by 1.5e-7 in all
+        tol = 2.0 ** -22 * vals.abs().double()[fin] + torch.finfo(dtype).eps * want[fin].abs() + torch.finfo(dtype).tiny
+        assert ((row[fin] - want[fin]).abs() <= tol).all()
+
+
 def test_linear_int8_sums_are_exact():
     """The largest products an int8 row can make: the sum is a 32-bit integer, rounded once."""
     K = 131056
@@ -303,6 +353,8 @@ def test_verify_trees(with_probs, kind, n, rows, vocab, lo, hi):
     tokens = drafted(rng, logits, parent, probs, lo, hi)
     n_rows = torch.from_numpy(rng.integers(1, rows + 1, n)).int()
     met = 0
+    if n > 2:
+        n_rows[0], n_rows[1] = -3, 1000                              # taken as 1 and as all
     for seed in range(4):
         u = torch.rand(n, rows, generator=_gen(seed))
         kw = dict(temperature=(1.0, 0.8, 0.3, 1.7)[seed], draft_probs=probs, lo=lo, hi=hi)

@@ -279,5 +279,11 @@ def test_context_call_refuses(c0, wcuda):
         gpu.verify_tree_sampled([0], [t], u[:4])
     with pytest.raises(ValueError):
         gpu.verify_tree_sampled([0], [t], u.cpu())
+    from paper_2507_22424_b200.binding import make_shape
+    n = len(gpu.draft_tree([0], make_shape((2, 2), (1, 2)))[0]["tokens"])
+    for other in (n - 1, n + 1):                                      # numbers for more or fewer rows than the device's tree has
+        with pytest.raises(SpecVLAError) as e:
+            gpu.verify_tree_sampled([0], None, torch.rand(other).cuda())
+        assert e.value.code == -1
     gpu.verify_tree_sampled([0], [t], u)                              # the context is as it was
     gpu.close()

@@ -25,7 +25,7 @@ VERIFY = dict(n_seq=2, rows=8, vocab=100, lo=0, hi=100, logits_type=0, logits=P,
 
 
 @pytest.mark.parametrize("change", [
-    dict(rows=0), dict(rows=-1), dict(d=0), dict(type=3), dict(type=4), dict(type=7), dict(code_type=0), dict(code_type=5), dict(x=0), dict(codes=0),
+    dict(rows=0), dict(rows=-1), dict(d=0), dict(d=(1 << 30) + 1, **{k: 1 << 31 for k in ("ldx", "ld_residual", "ld_sum", "ld_codes")}), dict(type=3), dict(type=4), dict(type=7), dict(code_type=0), dict(code_type=5), dict(x=0), dict(codes=0),
     dict(scale=0), dict(ldx=31), dict(ld_codes=31), dict(ld_residual=31), dict(ld_sum=31), dict(eps=-1e-6), dict(eps=float("nan")),
     dict(x=P + 1), dict(residual=P + 1), dict(sum=P + 1), dict(gain=P + 2), dict(scale=P + 2)])
 def test_norm_refuses(B, change):
@@ -48,7 +48,7 @@ def test_quantize_rows_refuses(B, args):
     dict(T=0), dict(N=0), dict(K=0), dict(T=-3), dict(type=0), dict(type=5), dict(out_type=3), dict(act=-1), dict(act=5), dict(X=0), dict(W=0),
     dict(Y=0), dict(status=0), dict(ldx=63), dict(ldw=63), dict(ldx=65), dict(ldw=68), dict(X=P + 8), dict(W=P + 2), dict(ldy=63),
     dict(ld_residual=63), dict(x_scale=P), dict(w_scale=P), dict(Y=P + 1), dict(residual=P + 1), dict(bias=P + 1), dict(status=P + 2),
-    dict(type=3, K=131072, ldx=131072, ldw=131072), dict(type=3, ldx=72), dict(type=4, x_scale=P + 2)])
+    dict(type=3, K=131072, ldx=131072, ldw=131072), dict(K=(1 << 29) + 8, ldx=1 << 30, ldw=1 << 30), dict(type=3, ldx=72), dict(type=4, x_scale=P + 2)])
 def test_linear_refuses(B, change):
     assert B.lib.specvla_linear(B.LINEAR_ARGS.pack(*{**LINEAR, **change}.values()), None) == INVALID
 
@@ -83,7 +83,7 @@ def test_verify_refuses_scratch(B):
 
 
 def test_context_call_refuses_null(B):
-    assert B.lib.specvla_verify_tree_sampled(None, 1, None, None, 1.0, None, None, None, None, None) == INVALID
+    assert B.lib.specvla_verify_tree_sampled(None, 1, None, None, 1.0, None, None, 5, None, None, None) == INVALID
 
 
 def test_argument_blocks_have_the_sizes_of_the_structures(B):
