@@ -7,8 +7,13 @@
 // and are decided as 64-bit arithmetic decides them. What 32 bits give is off by less than 2^-21 of itself, so
 // only values that near to the middle between two codes (about one in 10,000) are done again in 64 bits.
 //
-// One CTA per row, the row in registers between the reduction and the rounding: every input is read once and
-// every output written once. Bound by HBM at many rows, by launch and two dependent loads at few.
+// The row is in registers between the reduction and the rounding: every input is read once and every output written once.
+// What a row costs beside its bytes is a chain: loads, a reduction over the CTA, the factor, the codes. So it has one
+// block barrier and no 64-bit arithmetic on its way (the codes that stay open are settled afterwards by their warp alone:
+// with the row's largest value in 64 bits and a second barrier, 4764 rows of 4096 took 69 us, with both but fewer
+// instructions 57), 32 elements a thread (51 with 16) and the next row's copies in flight (47). 4764 x 4096 f32 with a residual
+// to e4m3: 47 us, 5.4 TB/s, bound by HBM; bf16: 26 us. 27 x 4096 bf16: 4.0 us, a launch and three dependent loads. 777 x 4095
+// f16, whose rows no 16-byte load fits: 10 us, one element per load.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

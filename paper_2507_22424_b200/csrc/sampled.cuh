@@ -13,10 +13,14 @@
 // in about one call of a hundred. exp is a table of 64 powers of two and a polynomial (Tang 1989), 10
 // 64-bit operations, so that a pass over logits stays near the rate at which they are read.
 //
-// Two launches. stats: a warp per (row, 512 ids) leaves their maximum and their sum of exponentials: all rows at
-// once, bound by HBM. walk: per tree one CTA (a cluster of eight, when a refused child asks for a pass over the
-// vocabulary); rows' sums and the children's weights are gathered in parallel, so that the walk itself runs from
-// shared memory, and the drawn token takes a search over the sums of 512 ids and one warp's scan.
+// Two launches. stats: a warp per (row, 512 ids) leaves their maximum and their sum of exponentials, all rows at once:
+// 22 us for 13.5 M f32 logits (816 rows of 32064 ids, half of them in ragged trees), 20 us for 12.3 M bf16 ones. Its bytes
+// take 8 and 4 us; it issues about 27 instructions a logit, 11 of them 64-bit, and is bound by that. walk: per tree one
+// CTA, or with draft probabilities a cluster of up to eight that shares the passes over the vocabulary which refused children
+// ask for; rows' sums and the children's weights are gathered in parallel, and without draft probabilities every child is
+// decided at once, so that the walk itself runs from shared memory; the drawn token takes a search over the sums of 512
+// ids and one warp's scan. One tree: 5 to 10 us, nearly all of it latency (dependent loads, 64-bit reductions). Both
+// together: 27 rows x 256 ids 11 us, 51 x 32064 16 us, 16 trees of 51 rows with draft probabilities 46 us, 64 chains 36 us.
 #pragma once
 #include <cooperative_groups.h>
 #include <algorithm>
