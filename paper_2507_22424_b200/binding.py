@@ -483,6 +483,8 @@ def _run(rc):
 def _codes_like(x, rows, d, dtype):
     """Codes of [rows, d], rows 16 bytes apart or a multiple of it, as linear() takes them; and that distance."""
     ld = (d + 15) & -16
+    if ld == d and x.is_contiguous():
+        return torch.empty_like(x, dtype=dtype), ld
     codes = x.new_empty((rows, ld), dtype=dtype)
     return (codes if ld == d else codes[:, :d]), ld
 
@@ -500,7 +502,7 @@ def rmsnorm_q8(x, gain=None, residual=None, eps=1e-6, dtype=torch.int8, out_sum=
     if residual is not None:
         same = (x.dtype,)
         ldr, res_p = _rows(residual, "residual", rows, d, same), residual.data_ptr()
-        total = x.new_empty((rows, d)) if out_sum is None else out_sum
+        total = torch.empty_like(x) if out_sum is None else out_sum
         lds, sum_p = _rows(total, "out_sum", rows, d, same), total.data_ptr()
     elif out_sum is not None:
         raise ValueError("out_sum without a residual")
@@ -621,7 +623,7 @@ def verify_sampled(logits, tokens, parent, u, n_rows=None, temperature=1.0, draf
     u_p = _whole(u, "u", torch.float32, shape)
     rows_p = 0 if n_rows is None else _whole(n_rows, "n_rows", torch.int32, (n,))
     dev = _device(logits, tokens, parent, u, n_rows, draft_probs)
-    m, path, out = tokens.new_empty(n), tokens.new_empty(shape), tokens.new_empty(shape)
+    m, path, out = tokens.new_empty(n), torch.empty_like(tokens), torch.empty_like(tokens)
     if n:
         nb = lib.specvla_verify_sampled_scratch_bytes(n, rows, lo, hi)
         if nb == 0:

@@ -13,14 +13,15 @@
 // in about one call of a hundred. exp is a table of 64 powers of two and a polynomial (Tang 1989), 10
 // 64-bit operations, so that a pass over logits stays near the rate at which they are read.
 //
-// Two launches. stats: a warp per (row, 512 ids) leaves their maximum and their sum of exponentials, all rows at once:
+// Two launches, or the second alone (LAZY, below). stats: a warp per (row, 512 ids) leaves their maximum and their sum of exponentials, all rows at once:
 // 22 us for 13.5 M f32 logits (816 rows of 32064 ids, half of them in ragged trees), 20 us for 12.3 M bf16 ones. Its bytes
 // take 8 and 4 us; it issues about 27 instructions a logit, 11 of them 64-bit, and is bound by that. walk: per tree one
 // CTA, or with draft probabilities a cluster of up to eight that shares the passes over the vocabulary which refused children
 // ask for; rows' sums and the children's weights are gathered in parallel, and without draft probabilities every child is
 // decided at once, so that the walk itself runs from shared memory; the drawn token takes a search over the sums of 512
 // ids and one warp's scan. One tree: 5 to 10 us, nearly all of it latency (dependent loads, 64-bit reductions). Both
-// together: 27 rows x 256 ids 11 us, 51 x 32064 16 us, 16 trees of 51 rows with draft probabilities 46 us, 64 chains 36 us.
+// together: 27 rows x 256 ids 11 us, 51 x 32064 15 us, 64 chains of 6 rows 36 us. Where the trees have many more rows than a walk
+// visits, the cluster sums a row when the walk comes to it: 16 trees of 51 rows with draft probabilities 39 us instead of 46.
 #pragma once
 #include <cooperative_groups.h>
 #include <algorithm>
@@ -155,6 +156,27 @@ template <typename T> __device__ __forceinline__ bool aligned4(const T *p) {
   return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
 }
 
+// Maximum and sum of exponentials of a piece (whole warp).
+template <typename T>
+__device__ __forceinline__ void sum_piece(const Args &a, const T *z0, int sub, int width, bool vec, const ExpTable &tab, float &m, double &s) {
+  float z[16];
+  load_piece<false>(z0, sub * SUB, width, vec, z);
+  m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 16; k++) m = fmaxf(m, z[k]);             // (a NaN loses)
+  m = warp_max(m);
+  const RowExp weight(m, a.temperature, a.factor);
+  s = 0.0;
+  if (m < INFINITY && weight.low < m) {
+#pragma unroll
+    for (int k = 0; k < 16; k++) s += weight.summand(z[k], tab);
+  } else if (m > -INFINITY) {                                  // infinite logits share the row, or the temperature is next to 0
+#pragma unroll
+    for (int k = 0; k < 16; k++) s += weight(z[k], tab);
+  }
+  s = warp_sum64(s);
+}
+
 // CTX: row numbers of a context's call (no rows are left out). A CTA takes a.per_cta pieces of one row, its warps in turn;
 // a warp asks for its next piece before it sums the present one.
 template <typename T, bool CTX>
@@ -174,21 +196,9 @@ static __global__ void __launch_bounds__(STATS_THREADS, 6) stats_kernel(const Ar
   const bool vec = aligned4(z0);
   __syncthreads();
   for (; sub < end; sub += STATS_THREADS / 32) {
-    float z[16], m = -INFINITY;
-    load_piece<false>(z0, sub * SUB, width, vec, z);
-#pragma unroll
-    for (int k = 0; k < 16; k++) m = fmaxf(m, z[k]);           // (a NaN loses)
-    m = warp_max(m);
-    const RowExp weight(m, a.temperature, a.factor);
-    double s = 0.0;
-    if (m < INFINITY && weight.low < m) {
-#pragma unroll
-      for (int k = 0; k < 16; k++) s += weight.summand(z[k], tab);
-    } else if (m > -INFINITY) {                                // infinite logits share the row, or the temperature is next to 0
-#pragma unroll
-      for (int k = 0; k < 16; k++) s += weight(z[k], tab);
-    }
-    s = warp_sum64(s);
+    float m;
+    double s;
+    sum_piece(a, z0, sub, width, vec, tab, m, s);
     if (lane == 0) {
       a.sub_max[(size_t)row * a.n_sub + sub] = m;
       a.sub_sum[(size_t)row * a.n_sub + sub] = s;
@@ -211,6 +221,7 @@ struct Walk {
   int n_refused, cur, next, m, want;      // want: the walk waits for a pass over the vocabulary
   double beta, S;
   double part[2][CLUSTER * WALK_THREADS / 32];   // sums of the cluster's warps, by turns
+  float part_max[2][CLUSTER * WALK_THREADS / 32];
 };
 
 // The piece at `target` of n sums (whole warp), and the cumulative sum before it; the last piece that has any weight
@@ -274,21 +285,23 @@ __device__ __forceinline__ int search_ids(double before, double target, int firs
   return some ? __shfl_sync(0xffffffffu, any, 31 - __clz(some)) : -1;
 }
 
-// Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends; PROBS: then p and q of the
-// first a.kept pieces of every warp.
-template <typename T, bool PROBS, bool CTX>
-static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kernel(const Args a, const EpArgs ea) {
+// LAZY: without the first launch; the cluster sums a row when the walk comes to it.
+// Dynamic shared memory: [n_sub] doubles, the sums of the pieces of the row where the walk ends; LAZY: [n_sub] floats, their
+// maxima; PROBS: then p and q of the first a.kept pieces of every warp.
+template <typename T, bool PROBS, bool LAZY, bool CTX>
+static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) walk_kernel(const Args a, const EpArgs ea) {
   namespace cg = cooperative_groups;
+  constexpr bool CLUSTERED = PROBS || LAZY;
   __shared__ ExpTable tab;
   __shared__ Walk w;
   extern __shared__ double s_sub[];
   fill(tab);
-  if (PROBS) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (that every CTA has started)
+  if (CLUSTERED) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (that every CTA has started)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int WARPS = WALK_THREADS / 32;
   if (tid < SV_MAX_TREE) w.inner[tid] = 0, w.parent[tid] = -1;
   int rank = 0, ranks = 1;
-  if (PROBS) {
+  if (CLUSTERED) {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   }
@@ -308,6 +321,9 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
     for (int k = lane; k < a.n_sub; k += 32) m = fmaxf(m, sm[k]);
     return warp_max(m);
   };
+
+  float *s_max = reinterpret_cast<float *>(s_sub + a.n_sub);
+  double *s_kept = s_sub + a.n_sub + (LAZY ? (a.n_sub + 1) / 2 : 0);
 
   // ---- the tree; a thread keeps its row's parent and token
   __syncthreads();
@@ -330,7 +346,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
   }
   __syncthreads();
   // ---- rows with children: maximum and sum from the pieces, a warp per row
-  for (int i = warp; i < n; i += WARPS) {
+  for (int i = warp; !LAZY && i < n; i += WARPS) {
     if (!w.inner[i]) continue;
     const float *sm = maxima_of(i);
     const double *su = sums_of(i);
@@ -362,9 +378,27 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
     return w.z[i] > 0.0 ? RowExp(w.zmax[i], a.temperature, a.factor)(z, tab) : x == 0 ? 1.0 : 0.0;
   };
   auto sum_of = [&](int i) { return w.z[i] > 0.0 ? w.z[i] : 1.0; };
-  if (tid < n) {
+  // weight of the thread's token in its parent's row
+  auto put_weight = [&]() {
     const double v = inside ? weight_of(my_parent, my_z, my_x) : 0.0;
     w.w[tid] = PROBS ? (inside ? v / sum_of(my_parent) : 0.0) : v;
+  };
+  // no PROBS: whether the thread's row is accepted if the walk comes to it; S: what is left of the parent's row then
+  auto put_yes = [&]() {
+    bool yes = false;
+    if (inside && !w.again[tid]) {
+      double S = sum_of(my_parent);
+#pragma unroll
+      for (int k = 0; k < 4; k++)
+        for (uint32_t left = elder[k]; left; left &= left - 1) {
+          const int j = 32 * k + __ffs(left) - 1;
+          if (!w.again[j]) S -= w.w[j];
+        }
+      yes = w.w[tid] > 0.0 && (double)w.u[tid] * S < w.w[tid];
+    }
+    w.yes[tid] = yes;
+  };
+  if (tid < n) {
     w.q[tid] = my_q;
     if (!PROBS) {
       // the row's elder siblings, a bit each
@@ -386,31 +420,69 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
         for (uint32_t left = elder[k]; left; left &= left - 1) again |= w.tok[32 * k + __ffs(left) - 1] == my_x;
       w.again[tid] = again;
     }
+    if (!LAZY) put_weight();
   }
   __syncthreads();
-  if (!PROBS) {
-    // what is left of the parent's row when the walk comes to this child: every child is decided at once
-    if (tid < n) {
-      bool yes = false;
-      if (inside && !w.again[tid]) {
-        double S = sum_of(my_parent);
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-          for (uint32_t left = elder[k]; left; left &= left - 1) {
-            const int j = 32 * k + __ffs(left) - 1;
-            if (!w.again[j]) S -= w.w[j];
-          }
-        yes = w.w[tid] > 0.0 && (double)w.u[tid] * S < w.w[tid];
-      }
-      w.yes[tid] = yes;
-    }
+  if (!PROBS && !LAZY) {                                         // every child is decided at once
+    if (tid < n) put_yes();
     __syncthreads();
   }
-  if (PROBS) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (CLUSTERED) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
   // ---- the walk: a warp runs it from shared memory, everybody joins for a pass over the vocabulary
   int turn = 0;
+  // Hands a value of this warp to the cluster's CTAs; all have all of them when it returns (the words of a turn are written
+  // again after the next hand-over, which every CTA comes to when it has read them).
+  auto hand_over = [&](double sum, float max) {
+    if (lane < ranks) {
+      cg::cluster_group cl = cg::this_cluster();
+      *cl.map_shared_rank(&w.part[turn][rank * WARPS + warp], lane) = sum;
+      if (LAZY) *cl.map_shared_rank(&w.part_max[turn][rank * WARPS + warp], lane) = max;
+    }
+    if (ranks > 1) cg::this_cluster().sync();
+    else __syncthreads();
+  };
+  bool fresh = true;                                             // LAZY: the walk has just come to its row
   for (;;) {
+    if constexpr (LAZY) {
+      if (fresh) {
+        const int cur = w.cur;
+        const T *z0 = logits_of(cur);
+        const bool vz = aligned4(z0);
+        float M = -INFINITY;
+        double S = 0.0;
+        for (int k = warp * ranks + rank; k < a.n_sub; k += WARPS * ranks) {
+          float m;
+          double s;
+          sum_piece(a, z0, k, width, vz, tab, m, s);
+          if (lane == 0) s_sub[k] = s, s_max[k] = m;
+          if (m > M) {
+            S = (M > -INFINITY ? S * RowExp(m, a.temperature, a.factor)(M, tab) : 0.0) + s;
+            M = m;
+          } else if (m > -INFINITY) {
+            S += s * RowExp(M, a.temperature, a.factor)(m, tab);
+          }
+        }
+        hand_over(S, M);
+        M = -INFINITY;
+        for (int k = lane; k < ranks * WARPS; k += 32) M = fmaxf(M, w.part_max[turn][k]);
+        M = warp_max(M);
+        const RowExp weight(M, a.temperature, a.factor);
+        S = 0.0;
+        for (int k = lane; k < ranks * WARPS; k += 32)
+          if (w.part_max[turn][k] > -INFINITY) S += w.part[turn][k] * weight(w.part_max[turn][k], tab);
+        S = warp_sum64(S);
+        turn ^= 1;
+        if (tid == 0) w.zmax[cur] = M, w.z[cur] = S;
+        __syncthreads();
+        if (tid < n && my_parent == cur) put_weight();
+        if (!PROBS) {
+          __syncthreads();
+          if (tid < n && my_parent == cur) put_yes();
+        }
+        __syncthreads();
+      }
+    }
     if (warp == 0) {
       int cur = w.cur, m = w.m;
       if constexpr (PROBS) {
@@ -430,6 +502,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
             m++;
             beta = 0.0, S = 1.0;
             if (lane == 0) w.path[m] = c;
+            if (LAZY) want = 4;                                  // its row's sum
           } else {
             // the sum of what is left: the row's first (1), with another child to come (3), a later one (2)
             unsigned others = 0;
@@ -441,7 +514,8 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
         }
         if (lane == 0) w.cur = cur, w.m = m, w.next = i0, w.beta = beta, w.S = S, w.want = want;
       } else {
-        for (int i0 = 1; i0 < n;) {
+        int want = 0;
+        for (int i0 = cur + 1; i0 < n && !want;) {
           const unsigned kids = __ballot_sync(0xffffffffu, i0 + lane < n && w.parent[i0 + lane] == cur && w.yes[i0 + lane]);
           if (!kids) {
             i0 += 32;
@@ -451,6 +525,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
           i0 = cur + 1;
           m++;
           if (lane == 0) w.path[m] = cur;
+          if (LAZY) want = 4;
         }
         // the children refused there
         int nref = 0;
@@ -461,11 +536,16 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
           if (no) w.refused[nref + __popc(all & ((1u << lane) - 1))] = w.tok[i];
           nref += __popc(all);
         }
-        if (lane == 0) w.cur = cur, w.m = m, w.n_refused = nref;
+        if (lane == 0) w.cur = cur, w.m = m, w.n_refused = nref, w.want = want;
       }
     }
     __syncthreads();
-    if (!PROBS || !w.want) break;
+    if (!CLUSTERED || !w.want) break;
+    fresh = w.want == 4;
+    if (LAZY && fresh) {
+      __syncthreads();                                           // (everyone has read what is wanted)
+      continue;
+    }
     if constexpr (PROBS) {
       // S = sum of max(p - beta q, 0): pieces go round the cluster's warps; their sums stay for the search, and p and q in
       // shared memory for the row's next pass
@@ -480,7 +560,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
       for (int k = warp * ranks + rank, n = 0; k < a.n_sub; k += WARPS * ranks, n++) {
         double p[16], s = 0.0;
         float q[16];
-        double *kp = s_sub + a.n_sub + ((size_t)n * WARPS + warp) * 768 + lane;   // 16 x 32 of p, then of q
+        double *kp = s_kept + ((size_t)n * WARPS + warp) * 768 + lane;   // 16 x 32 of p, then of q
         if (first || n >= a.kept) {
           float z[16];
           load_piece<false>(z0, k * SUB, width, vz, z);
@@ -507,9 +587,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
         if (lane == 0) s_sub[k] = s;
         mine += s;
       }
-      if (lane < ranks) *cg::this_cluster().map_shared_rank(&w.part[turn][rank * WARPS + warp], lane) = mine;
-      if (ranks > 1) cg::this_cluster().sync();
-      else __syncthreads();
+      hand_over(mine, 0.f);
       if (warp == 0) {
         double s = 0.0;
         for (int k = lane; k < ranks * WARPS; k += 32) s += w.part[turn][k];
@@ -524,25 +602,42 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
   // ---- the token after the path, from what is left of its last row
   const int cur = w.cur, m = w.m;
   const bool residual = PROBS && w.beta > 0.0 && w.S > 0.0;      // (the last pass was made with this beta)
-  if (PROBS && ranks > 1) {
+  if (CLUSTERED && ranks > 1) {
     // every CTA has its own pieces' sums: the first one collects them
     cg::cluster_group cl = cg::this_cluster();
-    if (residual && rank != 0)
+    if ((residual || LAZY) && rank != 0)
       for (int k = warp * ranks + rank; k < a.n_sub; k += WARPS * ranks)
-        if (lane == 0) cl.map_shared_rank(s_sub, 0)[k] = s_sub[k];
+        if (lane == 0) {
+          cl.map_shared_rank(s_sub, 0)[k] = s_sub[k];
+          if (LAZY) cl.map_shared_rank(s_max, 0)[k] = s_max[k];
+        }
     cl.sync();
     if (rank != 0) return;
   }
   const float *sm = maxima_of(cur);
   const double *su = sums_of(cur);
-  const float zm = w.inner[cur] ? w.zmax[cur] : row_max(sm);
+  const float zm = LAZY || w.inner[cur] ? w.zmax[cur] : row_max(sm);
   const RowExp weight(zm, a.temperature, a.factor);
   const bool none = !(zm > -INFINITY);
+  // the sums of p itself over the pieces first, first + step, ... (by warps, LAZY, from the logits; else by threads)
   auto plain_sums = [&](int first, int step) {
-    for (int k = first; k < a.n_sub; k += step) s_sub[k] = sm[k] > -INFINITY ? su[k] * weight(sm[k], tab) : 0.0;
+    if (LAZY) {
+      const T *z0 = logits_of(cur);
+      for (int k = first; k < a.n_sub; k += step) {
+        float m;
+        double s;
+        sum_piece(a, z0, k, width, aligned4(z0), tab, m, s);
+        if (lane == 0) s_sub[k] = m > -INFINITY ? s * weight(m, tab) : 0.0;
+      }
+    } else {
+      for (int k = first; k < a.n_sub; k += step) s_sub[k] = sm[k] > -INFINITY ? su[k] * weight(sm[k], tab) : 0.0;
+    }
   };
   if (!residual) {
-    plain_sums(tid, WALK_THREADS);
+    if (!LAZY) plain_sums(tid, WALK_THREADS);
+    else if (PROBS && w.beta > 0.0) plain_sums(warp, WARPS);     // (what was left there is nothing: the sums are gone)
+    else
+      for (int k = tid; k < a.n_sub; k += WALK_THREADS) s_sub[k] = s_max[k] > -INFINITY ? s_sub[k] * weight(s_max[k], tab) : 0.0;
     // pieces that hold a refused token are summed again without it
     for (int k0 = 0; !PROBS && k0 < w.n_refused; k0 += WARPS) {
       const int k = k0 + warp, piece = k < w.n_refused ? w.refused[k] / SUB : -1;
@@ -578,7 +673,8 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS ? 2 : 1) walk_kerne
     double total = sum_all();
     if (!none && !(total > 0.0) && drop) {                       // nothing is left: from p itself
       drop = 0;
-      plain_sums(lane, 32);
+      if (LAZY) plain_sums(0, 1);
+      else plain_sums(lane, 32);
       __syncwarp();
       total = sum_all();
     }
@@ -633,30 +729,42 @@ inline cudaError_t enqueue_t(Args a, const EpArgs &ea, int n_seq, int total_rows
   cfg.stream = st;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  // one piece a warp while there are few, up to three (816 rows of 32064 ids with their walk: 55 us, with one 58, with eight
-  // 61; 51 rows: 15, with two 16, with eight 22)
-  constexpr int WARPS = STATS_THREADS / 32;
-  const long long all = (long long)total_rows * a.n_sub, room = 148ll * 128;
-  a.per_cta = WARPS * (int)std::min(3ll, std::max(1ll, (all + room - 1) / room));
-  cfg.gridDim = dim3(total_rows, (a.n_sub + a.per_cta - 1) / a.per_cta);
-  cfg.blockDim = dim3(STATS_THREADS);
-  cudaError_t err = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a);
-  if (err != cudaSuccess) return err;
+  // All rows at once (a microsecond per 1150 pieces), unless they are many more than the walks visit: then row by row as they come
+  // to them, which is counted as six rows of every tree at 2.5 us beside their pieces. 16 trees of 51 rows of 32064 ids: 39 us, all at
+  // once 46; 64 chains of 6 rows: 47 and 36. (Paths that go on and on cost their rows.) A context's trees are few and small.
+  const bool lazy = !CTX && (long long)total_rows * a.n_sub > 6 * (2900 + (long long)n_seq * a.n_sub);
+  cudaError_t err = cudaSuccess;
+  if (!lazy) {
+    // one piece a warp while there are few, up to three (816 rows of 32064 ids with their walk: 55 us, with one 58, with eight
+    // 61; 51 rows: 15, with two 16, with eight 22)
+    constexpr int WARPS = STATS_THREADS / 32;
+    const long long all = (long long)total_rows * a.n_sub, room = 148 * 128;
+    a.per_cta = WARPS * (int)std::min(3ll, std::max(1ll, (all + room - 1) / room));
+    cfg.gridDim = dim3(total_rows, (a.n_sub + a.per_cta - 1) / a.per_cta);
+    cfg.blockDim = dim3(STATS_THREADS);
+    if ((err = cudaLaunchKernelEx(&cfg, stats_kernel<T, CTX>, a)) != cudaSuccess) return err;
+  }
   cfg.blockDim = dim3(WALK_THREADS);
-  cfg.dynamicSmemBytes = a.n_sub * sizeof(double);
+  cfg.dynamicSmemBytes = a.n_sub * sizeof(double) + (lazy ? (a.n_sub + 1) / 2 * sizeof(double) : 0);
   // a pass over the vocabulary is shared by as many CTAs as run at once, two on an SM
   int ranks = 1;
-  while (a.probs && ranks < CLUSTER && 2 * ranks * n_seq <= 2 * 148 && 2 * ranks <= a.n_sub) ranks *= 2;
+  while ((a.probs || lazy) && ranks < CLUSTER && 2 * ranks * n_seq <= 2 * 148 && 2 * ranks <= a.n_sub) ranks *= 2;
   constexpr size_t KEPT = WALK_THREADS / 32 * 768 * sizeof(double);   // bytes of one piece per warp
   a.kept = a.probs && a.n_sub <= WALK_THREADS / 32 * ranks ? 1 : 0;
   cfg.dynamicSmemBytes += a.kept * KEPT;
   cfg.gridDim = dim3(ranks * n_seq);
   at[1].val.clusterDim.x = ranks;
-  if (a.probs) cfg.numAttrs = 2;
-  if (a.kept && (err = cudaFuncSetAttribute(walk_kernel<T, true, CTX>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            (int)(MAX_IDS / SUB * sizeof(double) + KEPT))) != cudaSuccess)
-    return err;
-  return a.probs ? cudaLaunchKernelEx(&cfg, walk_kernel<T, true, CTX>, a, ea) : cudaLaunchKernelEx(&cfg, walk_kernel<T, false, CTX>, a, ea);
+  if (a.probs || lazy) cfg.numAttrs = 2;
+  auto go = [&](auto kernel) {
+    if (a.kept && (err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)(MAX_IDS / SUB * 12 + KEPT))) != cudaSuccess)
+      return err;
+    return cudaLaunchKernelEx(&cfg, kernel, a, ea);
+  };
+  if constexpr (!CTX) {
+    if (lazy) return a.probs ? go(walk_kernel<T, true, true, false>) : go(walk_kernel<T, false, true, false>);
+  }
+  return a.probs ? go(walk_kernel<T, true, false, CTX>) : go(walk_kernel<T, false, false, CTX>);
 }
 template <bool CTX>
 inline cudaError_t enqueue(const Args &a, const EpArgs &ea, int type, int n_seq, int total_rows, cudaStream_t st) {

@@ -105,7 +105,7 @@ def verify_sampled(logits, tokens, parent, u, n_rows=None, temperature=1.0, draf
                     continue
                 x = t[c] - lo
                 ok = 0 <= x < hi - lo
-                qx = 1.0 if q is None else (max(q[cur][t[c]], 0.0) if ok else 0.0)
+                qx = 1.0 if q is None else (q[cur][t[c]] if ok and q[cur][t[c]] > 0 else 0.0)      # (a NaN counts as 0)
                 if ok and left[x] > 0 and r[c] * qx * S < left[x]:
                     nxt = c
                     break

@@ -364,10 +364,46 @@ def test_verify_trees(with_probs, kind, n, rows, vocab, lo, hi):
     assert met > 0 or rows == 1 or (vocab == 32064 and not with_probs)
 
 
+@pytest.mark.parametrize("with_probs", [False, True])
+@pytest.mark.parametrize("kind,n,rows,vocab,lo,hi", [(F32, 6, 64, 32064, 0, 32064), (BF, 64, 64, 3000, 3, 2999), (HF, 400, 60, 600, 0, 600),
+                                                     (F32, 1500, 24, 500, 0, 500), (BF, 32, 128, 2100, 1, 2099)])
+def test_verify_many_rows(with_probs, kind, n, rows, vocab, lo, hi):
+    """More rows than are summed at once: rows are summed as the walk comes to them, by clusters of eight CTAs down to one."""
+    rng = np.random.default_rng(n + rows)
+    g = _gen(vocab)
+    logits = (_randn(g, n, rows, vocab) * 4).to(kind)
+    logits[0, 0] = math.nan                                          # nothing to draw from
+    logits[1, 0, lo + 5], logits[1, 0, hi - 1] = math.inf, math.inf
+    logits[2, 0, lo:hi] = -math.inf
+    logits[2, 0, hi - 1] = 1.0
+    parent = trees(rng, n, rows)
+    parent[3] = torch.tensor([-1] + list(range(rows - 1)))          # a chain
+    probs = None
+    if with_probs:
+        q = logits.float() + _randn(g, n, rows, vocab)
+        q[..., :lo], q[..., hi:] = -math.inf, -math.inf
+        probs = torch.softmax(q / 0.8, -1)                          # (NaN and zeros in the first trees' roots)
+    tokens = torch.zeros(n, rows, dtype=torch.int32)
+    top = torch.topk(torch.nan_to_num(logits[..., lo:hi].float(), nan=0.0), 6, dim=-1).indices + lo
+    for i in range(1, rows):
+        tokens[:, i] = top[torch.arange(n), parent[:, i].long(), torch.from_numpy(rng.integers(0, 6, n))]
+    n_rows = torch.from_numpy(rng.integers(1, rows + 1, n)).int()
+    met = 0
+    for seed in range(3):
+        u = torch.rand(n, rows, generator=_gen(seed))
+        kw = dict(temperature=(0.2, 1.0, 0.5)[seed], draft_probs=probs, lo=lo, hi=hi)
+        met += int(check_verify(logits, tokens, parent, u, **kw)[0].sum())
+        check_verify(logits, tokens, parent, u, n_rows=n_rows, **kw)
+    for fill in (0.0, 1.0 - 2.0 ** -24):
+        check_verify(logits, tokens, parent, torch.full((n, rows), fill), draft_probs=probs, lo=lo, hi=hi)
+    assert met > n
+
+
+@pytest.mark.parametrize("n", [3, 6])
 @pytest.mark.parametrize("kind", [F32, BF, HF])
-def test_verify_deep_paths_over_the_whole_vocabulary(kind):
+def test_verify_deep_paths_over_the_whole_vocabulary(kind, n):
     """Each row's likely tokens as its children, low temperatures: paths of many rows."""
-    n, rows, vocab = 3, 64, 32064
+    rows, vocab = 64, 32064
     g = _gen(77)
     logits = (_randn(g, n, rows, vocab) * 4).to(kind)
     parent = torch.tensor([-1] + [i // 2 * 2 for i in range(rows - 1)], dtype=torch.int32).repeat(n, 1)   # two children each
