@@ -134,6 +134,9 @@ inline uint32_t make_idesc(int kind, bool is_bf16, int m, int n) {
   const uint32_t fmt = kind == KIND_16 ? (is_bf16 ? 1u : 0u) : kind == KIND_I8 ? 1u : 0u;
   return ((kind == KIND_I8 ? 2u : 1u) << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+template <int KIND> __device__ __forceinline__ uint32_t add_acc(uint32_t a, uint32_t b) {
+  return KIND == KIND_I8 ? a + b : __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+}
 template <int KIND> __device__ __forceinline__ float acc_value(uint32_t r) {
   return KIND == KIND_I8 ? (float)(int)r : __uint_as_float(r);
 }
@@ -371,32 +374,49 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           if (a.bias) b[e] = a.bias[n + e];
         }
       const unsigned char *p0 = smem_raw + (base - smem_u32(smem_raw));
-      for (int t = rank + S * (et >> 6); t < T && one; t += 2 * S) {
-        float v[2];
-        if (KIND == KIND_I8) {
-          int s[2] = {0, 0};
-          for (int r = 0; r < S; r++) {
-            const int2 p = *reinterpret_cast<const int2 *>(cl.map_shared_rank(p0, r) + (t * BM + c) * 4);
-            s[0] += p.x, s[1] += p.y;
-          }
-          v[0] = (float)s[0], v[1] = (float)s[1];
-        } else {
-          v[0] = v[1] = 0.f;
-          for (int r = 0; r < S; r++) {
-            const float2 p = *reinterpret_cast<const float2 *>(cl.map_shared_rank(p0, r) + (t * BM + c) * 4);
-            v[0] += p.x, v[1] += p.y;
+      // four rows at a time, so that their loads (residual, then the S partial sums) are in flight together; past the last
+      // row and column the nearest element inside is read
+      for (int t0 = rank + S * (et >> 6); t0 < T; t0 += 8 * S) {
+        int t[4];
+        Two<OUT> r[4] = {};
+#pragma unroll
+        for (int u = 0; u < 4; u++) t[u] = min(t0 + 2 * S * u, T - 1);
+        if (res) {
+#pragma unroll
+          for (int u = 0; u < 4; u++) {
+            const OUT *q = res + (row0 + t[u]) * a.ldr;
+            if (a.pairs) r[u] = *reinterpret_cast<const Two<OUT> *>(q + min(n, a.N - 2));
+            else r[u].a = q[min(n, a.N - 1)], r[u].b = q[min(n + 1, a.N - 1)];
           }
         }
-        OUT *y = static_cast<OUT *>(a.y) + (row0 + t) * a.ldy + n;
-        for (int e = 0; e < 2; e++) v[e] = fmaf(v[e], sw[e] * s_scale[t], b[e]);
+        uint2 sum[4];
+        for (int o = 0; o < S; o++) {
+          const unsigned char *peer = cl.map_shared_rank(p0, o);
+          uint2 part[4];
+#pragma unroll
+          for (int u = 0; u < 4; u++) part[u] = *reinterpret_cast<const uint2 *>(peer + (t[u] * BM + c) * 4);
+#pragma unroll
+          for (int u = 0; u < 4; u++)
+            sum[u] = o == 0 ? part[u] : make_uint2(add_acc<KIND>(sum[u].x, part[u].x), add_acc<KIND>(sum[u].y, part[u].y));
+        }
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          v[2 * u] = fmaf(acc_value<KIND>(sum[u].x), sw[0] * s_scale[t[u]], b[0]);
+          v[2 * u + 1] = fmaf(acc_value<KIND>(sum[u].y), sw[1] * s_scale[t[u]], b[1]);
+        }
         activate<sizeof(OUT) == 2>(v, a.act);
-        for (int e = 0; e < 2; e++)
-          if (res && n + e < a.N) v[e] += as_float(res[(row0 + t) * a.ldr + n + e]);
-        if (two && a.pairs) {
-          put2(y, v[0], v[1]);
-        } else {
-          put(y, v[0]);
-          if (two) put(y + 1, v[1]);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          if (!one || t0 + 2 * S * u >= T) continue;
+          OUT *y = static_cast<OUT *>(a.y) + (row0 + t[u]) * a.ldy + n;
+          if (res) v[2 * u] += as_float(r[u].a), v[2 * u + 1] += as_float(r[u].b);
+          if (two && a.pairs) {
+            put2(y, v[2 * u], v[2 * u + 1]);
+          } else {
+            put(y, v[2 * u]);
+            if (two) put(y + 1, v[2 * u + 1]);
+          }
         }
       }
     }
@@ -620,17 +640,26 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       tc_fence_after();
       const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN);
       const int t_end = min((half + 1) * cols, T);
-      Two<OUT> next[8];                                         // the residual, 16 columns ahead
+      Two<OUT> next[8];                                         // residual and accumulator, 16 rows ahead
+      uint32_t ahead[16];
       residual16<OUT>(a, next, n, half * cols, T, row0);
+      if (half * cols < t_end) tc_ld16(ta + half * cols, ahead);
       for (int t0 = half * cols; t0 < t_end; t0 += 16) {
         uint32_t v[16];
-        tc_ld16(ta + t0, v);
         Two<OUT> r[8];
+        tc_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+          v[k] = ahead[k];
+          asm volatile("" : "+r"(v[k]));                        // (a copy: the next columns go to `ahead`)
+        }
 #pragma unroll
         for (int k = 0; k < 8; k++) r[k] = next[k];
         hold(r);
-        if (t0 + 16 < t_end) residual16<OUT>(a, next, n, t0 + 16, T, row0);
-        tc_wait_ld();
+        if (t0 + 16 < t_end) {
+          tc_ld16(ta + t0 + 16, ahead);
+          residual16<OUT>(a, next, n, t0 + 16, T, row0);
+        }
         finish16<KIND, OUT>(a, v, r, n, t0, T, row0, sw, b, s_scale[buf]);
       }
       tc_fence_before();

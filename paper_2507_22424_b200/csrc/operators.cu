@@ -141,21 +141,26 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   for (int s = 2; fit && s <= linear::MAX_S; s++)
     if ((long long)fit->clusters[s] >= (long long)p.tiles * p.chunks && KB / s >= 4) p.S = s;
   best = p;
-  // pairs of CTAs for more than 128 rows, and where the slices would take more than one round (27 x 32064 x 4096 in int8: 25.6 us
-  // as 251 slices of 128 columns on 148 SMs, 23.7 as 126 tiles of 256 on 74 pairs; 11008 columns, one round: the same)
-  if (fit && fit->clusters[2] > 0 && (T > 128 || (long long)p.tiles * p.chunks > fit->clusters[1])) {
+  // Clocks of a choice: K blocks, whose bytes come from L2 at 64 a clock and SM (slices: 256 + 2 tn, pairs: 256 + tn a block);
+  // start, accumulator and exit; slices' hand-over. Neither is done before the weights have been read, at 3440 bytes a clock.
+  const double read = (double)N * KB * linear::KBYTES / 3440 + 8000;
+  const long long rounds = p.S > 1 ? 1 : ((long long)p.tiles * p.chunks + std::max(1, fit ? fit->clusters[1] : 1) - 1) / std::max(1, fit ? fit->clusters[1] : 1);
+  double cost = rounds * (((KB + p.S - 1) / p.S) * (256. + 2 * p.tn) + 8000 + 24 * p.tn);
+  if (p.S > 1) cost += 2500 + (p.tn / (8 * p.S) + 1) * 1000;
+  cost = std::max(cost, read);
+  if (rounds > 1) cost *= 1.01;            // (27 x 32064 x 4096 in int8: 25.6 us as 251 slices on 148 SMs, 23.7 as 126 tiles on 74 pairs)
+  if (fit && fit->clusters[2] > 0 && T > 16) {
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
-    double cost = 1e30;
     const int cmin = (T + linear::MAX_TN - 1) / linear::MAX_TN;
     for (int c = cmin; c <= 8 * cmin + 4 && c <= T; c++) {
       const int tn = ((T + c - 1) / c + 31) / 32 * 32;
       if (tn > linear::MAX_TN || tn < 32) continue;
       const int chunks = (T + tn - 1) / tn;
       const long long waves = ((long long)tiles * chunks + pairs - 1) / pairs;
-      const double k = waves * (double)((double)KB * (256 + tn) + 8000 + 24 * tn);
+      const double k = std::max(read, waves * (KB * (256. + tn) + 8000 + 24 * tn));
       if (k < cost) {
         cost = k;
-        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2};
+        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2, 0};
       }
     }
   }
