@@ -287,3 +287,61 @@ def test_context_call_refuses(c0, wcuda):
         assert e.value.code == -1
     gpu.verify_tree_sampled([0], [t], u)                              # the context is as it was
     gpu.close()
+
+
+def test_rows_further_apart_than_32_bits_count():
+    """Two rows 2^31 elements apart, in every operand whose rows have a distance."""
+    B = _b()
+    far = 2 ** 31
+    big = torch.empty(far + 128, dtype=torch.float16, device="cuda")
+    rows = big.as_strided((2, 96), (far, 1))
+    g = torch.Generator().manual_seed(3)
+    x, w = torch.randn(2, 96, generator=g).half().cuda(), torch.randn(80, 96, generator=g).half().cuda()
+    rows.copy_(x)
+    want = B.rmsnorm_q8(x, residual=x, dtype=torch.float8_e4m3fn)
+    got = B.rmsnorm_q8(rows, residual=rows, dtype=torch.float8_e4m3fn)
+    assert all(torch.equal(a.float(), b.float()) for a, b in zip(got, want))
+    y = B.linear(x, w)
+    assert torch.equal(B.linear(rows, w), y)
+    assert torch.equal(B.linear(w, rows), B.linear(w, x))
+    out = big.as_strided((2, 80), (far, 1))
+    rows.copy_(x)
+    out.copy_(y)
+    assert torch.equal(B.linear(x, w, residual=out, out=out), B.linear(x, w, residual=y))
+    parent, u = torch.tensor([[-1, 0]], dtype=torch.int32).cuda(), torch.tensor([[0.7, 0.0]]).cuda()
+    rows.copy_(x)
+    tokens = torch.tensor([[0, 17]], dtype=torch.int32).cuda()
+    assert all(torch.equal(a, b) for a, b in zip(B.verify_sampled(rows[None], tokens, parent, u), B.verify_sampled(x[None], tokens, parent, u)))
+    del big, rows, out
+    torch.cuda.empty_cache()
+
+
+def test_two_host_threads_at_once():
+    import threading
+    B = _b()
+    tails = [Tail(), Tail(torch.float8_e4m3fn)]
+    for t in tails:
+        t()
+    torch.cuda.synchronize()
+    outs, errors = [[], []], []
+
+    def work(k):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(30):
+                    outs[k].append(tails[k]())
+                B.linear_status()
+        except Exception as e:                                        # reported by the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for k in range(2):
+        check_tail(tails[k], outs[k][0])
+        for out in outs[k][1:]:
+            assert all(torch.equal(a, b) for a, b in zip(out, outs[k][0]))
