@@ -58,9 +58,6 @@ __device__ __forceinline__ void put(__half *p, float v) { *p = __float2half(v); 
 __device__ __forceinline__ void put2(float *p, float a, float b) { *reinterpret_cast<float2 *>(p) = make_float2(a, b); }
 __device__ __forceinline__ void put2(bf16 *p, float a, float b) { *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b); }
 __device__ __forceinline__ void put2(__half *p, float a, float b) { *reinterpret_cast<__half2 *>(p) = __floats2half2_rn(a, b); }
-__device__ __forceinline__ float2 get2(const float *p) { return *reinterpret_cast<const float2 *>(p); }
-__device__ __forceinline__ float2 get2(const bf16 *p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(p)); }
-__device__ __forceinline__ float2 get2(const __half *p) { return __half22float2(*reinterpret_cast<const __half2 *>(p)); }
 
 // FAST: for results that are rounded to 16 bits. exp2 and the reciprocal of the special-function unit (2^-22 relative)
 // in place of expf and a division; tanh through v / (1 + exp(-2z)), which cancels nothing.
@@ -145,25 +142,43 @@ __host__ __device__ constexpr int stages_of(int tn) { return RING / stage_bytes(
 __host__ __device__ constexpr int tmem_cols(int tn) { return tn <= 32 ? 32 : tn <= 64 ? 64 : tn <= 128 ? 128 : 256; }
 
 template <typename OUT> struct alignas(2 * sizeof(OUT)) Two { OUT a, b; };
-// The residual of 16 accumulator columns (rows t0 .. t0 + 15 of the chunk) of this lane's output column n, as finish16
-// adds it: asked for ahead of the accumulator. No branch and no conversion here (what lies outside is read from the
-// nearest element inside): behind either, every load would wait for the one before it (1001 x 4332 x 2056 in f16:
+// One element, or two side by side, into the low bits of r (two floats: r and r1); r keeps its value where p is false. A
+// predicated load, not a branch: behind a branch, every load would wait for the one before it (1001 x 4332 x 2056 in f16:
 // 54 us instead of 24).
+template <int BYTES> __device__ __forceinline__ void load_if(uint32_t &r, uint32_t &r1, const void *q, bool p) {
+  if constexpr (BYTES == 2)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+r"(r) : "l"(q), "r"((int)p));
+  else if constexpr (BYTES == 4)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(r) : "l"(q), "r"((int)p));
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}"
+                 : "+r"(r), "+r"(r1) : "l"(q), "r"((int)p));
+}
+__device__ __forceinline__ uint32_t pack2(bf16, float a, float b) { const __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ uint32_t pack2(__half, float a, float b) { const __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ float2 unpack2(bf16, uint32_t r) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&r)); }
+__device__ __forceinline__ float2 unpack2(__half, uint32_t r) { return __half22float2(*reinterpret_cast<const __half2 *>(&r)); }
+template <typename OUT> __device__ __forceinline__ float unpack1(uint32_t r) {
+  if constexpr (sizeof(OUT) == 4) return __uint_as_float(r);
+  else return unpack2(OUT{}, r).x;
+}
+
+// The residual of 16 accumulator columns (rows t0 .. t0 + 15 of the chunk) of this lane's output column n, asked for ahead of
+// the accumulator. In pairs: of the row t0 + 2 p + (n & 1) two columns, r[p] (floats: r[2 p], r[2 p + 1]).
 template <typename OUT>
-__device__ __forceinline__ void residual16(const Args &a, Two<OUT> (&r)[8], int n, int t0, int T, long long row0) {
-  const OUT *res = static_cast<const OUT *>(a.res);
-  if (!res) return;
+__device__ __forceinline__ void residual16(const Args &a, uint32_t (&r)[16], int n, int t0, int T, long long row0) {
+  if (!a.res) return;
+  const OUT *q = static_cast<const OUT *>(a.res);
   if (a.pairs) {
-    res += row0 * a.ldr + min(n & ~1, a.N - 2);
+    const int odd = n & 1, ne = n & ~1, left = ne < a.N ? T - t0 - odd : 0;
+    q += (row0 + t0 + odd) * a.ldr + ne;
 #pragma unroll
-    for (int p = 0; p < 8; p++) r[p] = *reinterpret_cast<const Two<OUT> *>(res + min(t0 + 2 * p + (n & 1), T - 1) * a.ldr);
+    for (int p = 0; p < 8; p++, q += 2 * a.ldr) load_if<2 * sizeof(OUT)>(r[sizeof(OUT) == 2 ? p : 2 * p], r[2 * p + 1], q, 2 * p < left);
   } else {
-    res += row0 * a.ldr + min(n, a.N - 1);
+    const int left = n < a.N ? T - t0 : 0;
+    q += (row0 + t0) * a.ldr + n;
 #pragma unroll
-    for (int p = 0; p < 8; p++) {
-      r[p].a = res[min(t0 + 2 * p, T - 1) * a.ldr];
-      r[p].b = res[min(t0 + 2 * p + 1, T - 1) * a.ldr];
-    }
+    for (int j = 0; j < 16; j++, q += a.ldr) load_if<sizeof(OUT)>(r[j], r[j], q, j < left);
   }
 }
 // Asks for the residual of a tile's 128 columns from n0 in L2, long before it is added: thread i of `threads` takes rows
@@ -178,51 +193,77 @@ __device__ __forceinline__ void prefetch_residual(const Args &a, int i, int thre
     asm volatile("prefetch.global.L2 [%0];" ::"l"(q + last));
   }
 }
-// Values that are not looked at before this point: without it the conversion to fp32 moves up to the loads, and each waits for
-// its own.
-__device__ __forceinline__ void hold(Two<float> (&r)[8]) {
+// Values that are not looked at before this point: without it their use moves up to the loads, and each waits for its own.
+__device__ __forceinline__ void hold(uint32_t (&r)[16]) {
 #pragma unroll
-  for (int k = 0; k < 8; k++) asm volatile("" : "+f"(r[k].a), "+f"(r[k].b));
+  for (int k = 0; k < 16; k++) asm volatile("" : "+r"(r[k]));
 }
-template <typename OUT> __device__ __forceinline__ void hold(Two<OUT> (&r)[8]) {
+__device__ __forceinline__ void hold(float (&r)[16]) {
 #pragma unroll
-  for (int k = 0; k < 8; k++)
-    asm volatile("" : "+h"(*reinterpret_cast<unsigned short *>(&r[k].a)), "+h"(*reinterpret_cast<unsigned short *>(&r[k].b)));
+  for (int k = 0; k < 16; k++) asm volatile("" : "+f"(r[k]));
 }
-// Finishes and stores these 16 columns: v is the accumulator. In pairs, neighbouring lanes exchange a value each per
-// two rows, so that both store two columns of one row: half as many stores.
-template <int KIND, typename OUT>
-__device__ __forceinline__ void finish16(const Args &a, const uint32_t (&acc)[16], const Two<OUT> (&r)[8], int n, int t0, int T,
-                                         long long row0, float sw, float b, const float *s_scale) {
-  float v[16];
+// 16 accumulator columns (rows t0 .. t0 + 15) of one output column: scales and bias. `acc` is free afterwards, for the next columns.
+template <int KIND>
+__device__ __forceinline__ void scale16(const Args &a, const uint32_t (&acc)[16], float (&v)[16], float sw, float b, const float *s_scale) {
+  if (a.x_scale) {
 #pragma unroll
-  for (int j = 0; j < 16; j += 4) {
-    const float4 sx = *reinterpret_cast<const float4 *>(s_scale + t0 + j);
-    v[j] = fmaf(acc_value<KIND>(acc[j]), sw * sx.x, b);
-    v[j + 1] = fmaf(acc_value<KIND>(acc[j + 1]), sw * sx.y, b);
-    v[j + 2] = fmaf(acc_value<KIND>(acc[j + 2]), sw * sx.z, b);
-    v[j + 3] = fmaf(acc_value<KIND>(acc[j + 3]), sw * sx.w, b);
+    for (int j = 0; j < 16; j += 4) {
+      const float4 sx = *reinterpret_cast<const float4 *>(s_scale + j);
+      v[j] = fmaf(acc_value<KIND>(acc[j]), sw * sx.x, b);
+      v[j + 1] = fmaf(acc_value<KIND>(acc[j + 1]), sw * sx.y, b);
+      v[j + 2] = fmaf(acc_value<KIND>(acc[j + 2]), sw * sx.z, b);
+      v[j + 3] = fmaf(acc_value<KIND>(acc[j + 3]), sw * sx.w, b);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; j++) v[j] = fmaf(acc_value<KIND>(acc[j]), sw, b);
   }
+}
+// Finishes and stores them. In pairs, neighbouring lanes exchange their values of every second row, so that both store two
+// columns of one row: half as many stores. 16-bit results are exchanged rounded, two rows in one register; their residual,
+// read in the order of the stores, goes the other way first (one exchange and one byte permutation are their own inverse).
+template <typename OUT>
+__device__ __forceinline__ void finish16(const Args &a, float (&v)[16], const uint32_t (&r)[16], int n, int t0, int T, long long row0) {
   activate<sizeof(OUT) == 2>(v, a.act);
   OUT *y = static_cast<OUT *>(a.y);
   if (a.pairs) {
-    const bool odd = n & 1;
-    const int ne = n & ~1;
-    OUT *q = y + (row0 + t0 + (odd ? 1 : 0)) * a.ldy + ne;
+    const int odd = n & 1, ne = n & ~1, left = ne < a.N ? T - t0 - odd : 0;
+    OUT *q = y + (row0 + t0 + odd) * a.ldy + ne;
+    if constexpr (sizeof(OUT) == 2) {
+      const uint32_t order = odd ? 0x3276 : 0x5410;
+      if (a.res) {
 #pragma unroll
-    for (int p = 0; p < 8; p++, q += 2 * a.ldy) {
-      const float other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * p] : v[2 * p + 1], 1);
-      float lo = odd ? other : v[2 * p], hi = odd ? v[2 * p + 1] : other;
-      if (a.res) lo += as_float(r[p].a), hi += as_float(r[p].b);
-      if (t0 + 2 * p + (odd ? 1 : 0) < T && ne < a.N) put2(q, lo, hi);
+        for (int p = 0; p < 8; p++) {
+          const float2 f = unpack2(OUT{}, __byte_perm(r[p], __shfl_xor_sync(0xffffffffu, r[p], 1), order));
+          v[2 * p] += f.x;
+          v[2 * p + 1] += f.y;
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < 8; p++, q += 2 * a.ldy) {
+        const uint32_t w = pack2(OUT{}, v[2 * p], v[2 * p + 1]);
+        const uint32_t w2 = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), order);
+        if (2 * p < left) *reinterpret_cast<uint32_t *>(q) = w2;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 8; p++, q += 2 * a.ldy) {
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * p] : v[2 * p + 1], 1);
+        float lo = odd ? other : v[2 * p], hi = odd ? v[2 * p + 1] : other;
+        if (a.res) lo += unpack1<OUT>(r[2 * p]), hi += unpack1<OUT>(r[2 * p + 1]);
+        if (2 * p < left) put2(q, lo, hi);
+      }
     }
   } else {
+    const int left = n < a.N ? T - t0 : 0;
     OUT *q = y + (row0 + t0) * a.ldy + n;
+    if (a.res) {
 #pragma unroll
-    for (int j = 0; j < 16; j++, q += a.ldy) {
-      if (a.res) v[j] += as_float(j & 1 ? r[j / 2].b : r[j / 2].a);
-      if (t0 + j < T && n < a.N) put(q, v[j]);
+      for (int j = 0; j < 16; j++) v[j] += unpack1<OUT>(r[j]);
     }
+#pragma unroll
+    for (int j = 0; j < 16; j++, q += a.ldy)
+      if (j < left) put(q, v[j]);
   }
 }
 
@@ -343,11 +384,14 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         uint32_t v[16];
         tc_ld16(ta + t0, v);
         if (S == 1) {
-          Two<OUT> r[8];
+          uint32_t r[16] = {};
           residual16<OUT>(a, r, n, t0, T, row0);
-          hold(r);
           tc_wait_ld();
-          finish16<KIND, OUT>(a, v, r, n, t0, T, row0, sw, b, s_scale);
+          hold(v);
+          hold(r);
+          float f[16];
+          scale16<KIND>(a, v, f, sw, b, s_scale + t0);
+          finish16<OUT>(a, f, r, n, t0, T, row0);
         } else {
           tc_wait_ld();
 #pragma unroll
@@ -539,8 +583,6 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  if (!a.x_scale)
-    for (int t = threadIdx.x; t < 2 * MAX_TN; t += PAIR_THREADS) (&s_scale[0][0])[t] = 1.f;
   tc_fence_before();
   __syncthreads();
   cooperative_groups::this_cluster().sync();                   // the peer's barriers and tensor memory are there too
@@ -640,27 +682,24 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       tc_fence_after();
       const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN);
       const int t_end = min((half + 1) * cols, T);
-      Two<OUT> next[8];                                         // residual and accumulator, 16 rows ahead
-      uint32_t ahead[16];
+      uint32_t acc[16], next[16] = {};                          // accumulator and residual, 16 rows ahead
       residual16<OUT>(a, next, n, half * cols, T, row0);
-      if (half * cols < t_end) tc_ld16(ta + half * cols, ahead);
+      if (half * cols < t_end) tc_ld16(ta + half * cols, acc);
       for (int t0 = half * cols; t0 < t_end; t0 += 16) {
-        uint32_t v[16];
-        Two<OUT> r[8];
+        uint32_t r[16];
+        float v[16];
         tc_wait_ld();
+        hold(acc);
+        scale16<KIND>(a, acc, v, sw, b, s_scale[buf] + t0);
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-          v[k] = ahead[k];
-          asm volatile("" : "+r"(v[k]));                        // (a copy: the next columns go to `ahead`)
-        }
-#pragma unroll
-        for (int k = 0; k < 8; k++) r[k] = next[k];
+        for (int k = 0; k < 16; k++) r[k] = next[k];
+        hold(v);
         hold(r);
         if (t0 + 16 < t_end) {
-          tc_ld16(ta + t0 + 16, ahead);
+          tc_ld16(ta + t0 + 16, acc);
           residual16<OUT>(a, next, n, t0 + 16, T, row0);
         }
-        finish16<KIND, OUT>(a, v, r, n, t0, T, row0, sw, b, s_scale[buf]);
+        finish16<OUT>(a, v, r, n, t0, T, row0);
       }
       tc_fence_before();
       __syncwarp();
