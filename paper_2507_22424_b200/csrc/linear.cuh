@@ -70,19 +70,30 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_times(float v, flo
   }
   return v / (1.f + expf(-z));
 }
-// v / 2 erfc(-v / sqrt 2) with erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), off by at most 1.5e-7
-// (Abramowitz and Stegun 7.1.26); negative v take the small product itself, so that nothing cancels.
-__device__ __forceinline__ float fast_gelu(float v) {
-  const float x = fabsf(v) * 0.70710678f;
-  float e, t;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-1.442695041f * x * x));
-  asm("rcp.approx.f32 %0, %1;" : "=f"(t) : "f"(fmaf(0.3275911f, x, 1.f)));
-  float p = fmaf(t, 1.061405429f, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f) * t;
-  const float q = p * e, y = 0.5f * v * q;
-  return v > 0.f ? (q > 0.f ? v - y : v) : y;                  // (infinity stays one)
+// max(v, 0) - |v| / 2 erfc(|v| / sqrt 2) with erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), off by at
+// most 1.5e-7 (Abramowitz and Stegun 7.1.26; the constants here are a_k / 2 and those for |v| in place of x); negative v
+// take the small product itself, so that nothing cancels. Two at a time: both reciprocals come from the one of their product
+// (the special-function unit takes 8 clocks an instruction). |v| stops at 64, where the product is long 0, so that
+// everything stays in range, and 0 v keeps the NaN of a NaN and of -infinity. No branch on v: 15 us instead of 11 for
+// 1001 x 4331 x 128.
+__device__ __forceinline__ void fast_gelu(float &v0, float &v1) {
+  const float m[2] = {fminf(fabsf(v0), 64.f), fminf(fabsf(v1), 64.f)};
+  const float d0 = fmaf(0.23164189f, m[0], 1.f), d1 = fmaf(0.23164189f, m[1], 1.f);
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+  const float t[2] = {r * d1, r * d0};
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    float &v = k ? v1 : v0;
+    float e;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-0.72134752f * m[k] * m[k]));
+    float p = fmaf(t[k], 0.5307027145f, -0.7265760135f);
+    p = fmaf(p, t[k], 0.7107068705f);
+    p = fmaf(p, t[k], -0.142248368f);
+    p = fmaf(p, t[k], 0.127414796f) * t[k];
+    const float flat = 0.f * v, base = v > 0.f ? v : flat;
+    v = fmaf(-m[k], p * e, base);
+  }
 }
 template <bool FAST, int M> __device__ __forceinline__ void activate(float (&v)[M], int act) {
   switch (act) {
@@ -91,8 +102,13 @@ template <bool FAST, int M> __device__ __forceinline__ void activate(float (&v)[
       for (int j = 0; j < M; j++) v[j] = v[j] < 0.f ? 0.f : v[j];         // (a NaN stays one)
       break;
     case ACT_GELU:
+      if constexpr (FAST) {
 #pragma unroll
-      for (int j = 0; j < M; j++) v[j] = FAST ? fast_gelu(v[j]) : 0.5f * v[j] * (1.f + erff(v[j] * 0.70710678f));
+        for (int j = 0; j < M; j += 2) fast_gelu(v[j], v[j + 1]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < M; j++) v[j] = 0.5f * v[j] * (1.f + erff(v[j] * 0.70710678f));
+      }
       break;
     case ACT_GELU_TANH:
       // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (v + 0.044715 v^3)
