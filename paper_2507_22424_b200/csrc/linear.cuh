@@ -283,8 +283,8 @@ __device__ __forceinline__ void finish16(const Args &a, float (&v)[16], const ui
   }
 }
 
-// Few rows: bound by the weights. One row by 4096 x 4096 in bf16 9.4 us (32 tiles of four CTAs; 5.1 us of weights, the rest start,
-// first loads and the hand-over between CTAs), 27 x 11008 x 4096 18.8 us (86 CTAs, 4.8 TB/s).
+// Few rows: bound by the weights. One row by 4096 x 4096 in bf16 9.7 us (32 tiles of four CTAs; 5.1 us of weights, the rest start,
+// first loads and the hand-over between CTAs), 27 x 11008 x 4096 18.2 us (86 CTAs, 5.0 TB/s).
 // One tile of 128 columns by one chunk of rows per cluster of S CTAs, which share its K blocks. S = 1: finished from
 // tensor memory. S > 1: every CTA leaves its partial tile in its own shared memory, and after one cluster barrier
 // finishes the rows rank, rank + S, ... from all of them, in rank order (the result does not depend on timing).
@@ -500,8 +500,9 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 // every n-th tile; the accumulator has two buffers in tensor memory, and eight warps finish one tile while the
 // tensor cores work on the next. A K block of tn rows takes 256 + tn clocks, its bytes at 64 a clock and SM; its MMAs take
 // 2 tn. 4764 x 22016 x 4096 in e4m3 293 us, 2.93 PFLOP/s (the tensor pipe 88 % of the time, clocks at the power limit);
-// 4096^3 in bf16 95 us, 1.45 PFLOP/s; 290 x 11008 x 4096 in bf16 30 us (32 with GELU; 129 tiles on 74 pairs, bound by L2);
-// the int8 head of 27 rows (32064 x 4096) 23.6 us, 5.7 TB/s.
+// 4096^3 in bf16 93 us, 1.47 PFLOP/s; 290 x 11008 x 4096 in bf16 30 us (32 with GELU; 129 tiles on 74 pairs, bound by L2);
+// the int8 head of 27 rows (32064 x 4096) 23.7 us, 5.7 TB/s. Where K is short the finishing loop counts: 2000 x 4096 x 512 in
+// bf16 12.0 us, 2368 x 4096 x 128 11.7 us.
 constexpr int PAIR_THREADS = 320;          // warp 0 copies, warp 1 MMAs (of the pair's first CTA), warps 2-9 epilogue
 constexpr int PAIR_STAGES = 8;
 __host__ __device__ constexpr int pair_stage(int tn) { return W_BYTES + tn / 2 * KBYTES; }

@@ -149,13 +149,12 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   if (p.S > 1) cost += 2500 + (p.tn / (8 * p.S) + 1) * 1000;
   cost = std::max(cost, read);
   if (rounds > 1) cost *= 1.01;            // (27 x 32064 x 4096 in int8: 25.6 us as 251 slices on 148 SMs, 23.7 as 126 tiles on 74 pairs)
+  if (p.chunks > 65535) cost = 1e300;      // (more than a grid's second dimension holds)
   if (fit && fit->clusters[2] > 0 && T > 16) {
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
-    const int cmin = (T + linear::MAX_TN - 1) / linear::MAX_TN;
-    for (int c = cmin; c <= 8 * cmin + 4 && c <= T; c++) {
-      const int tn = ((T + c - 1) / c + 31) / 32 * 32;
-      if (tn > linear::MAX_TN || tn < 32) continue;
+    for (int tn = linear::MAX_TN; tn >= 32; tn -= 32) {
       const int chunks = (T + tn - 1) / tn;
+      if (((T + chunks - 1) / chunks + 31) / 32 * 32 != tn) continue;    // (narrower chunks are no more)
       const long long waves = ((long long)tiles * chunks + pairs - 1) / pairs;
       const double k = std::max(read, waves * (KB * (256. + tn) + 8000 + 24 * tn));
       if (k < cost) {
@@ -259,7 +258,7 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   a.withhold = g_linear_withhold.exchange(0);
   const int kind = l->type == SPECVLA_I8 ? linear::KIND_I8 : l->type == SPECVLA_E4M3 ? linear::KIND_E4M3 : linear::KIND_16;
   const Plan p = plan_linear(l->T, l->N, a.KB, cluster_fit());
-  if (p.chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
+  if (!p.pair && p.chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
   a.tn = p.tn;
   a.idesc = linear::make_idesc(kind, l->type == SPECVLA_BF16, p.pair ? 2 * linear::BM : linear::BM, a.tn);
   CUtensorMap mw, mx;

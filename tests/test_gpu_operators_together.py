@@ -345,3 +345,13 @@ def test_two_host_threads_at_once():
         check_tail(tails[k], outs[k][0])
         for out in outs[k][1:]:
             assert all(torch.equal(a, b) for a, b in zip(out, outs[k][0]))
+
+
+def test_very_many_rows():
+    """More rows than 65535 chunks of 256."""
+    T = 65536 * 256 + 77
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randint(-3, 4, (T, 8), generator=g, device="cuda").half()
+    w = torch.randint(-3, 4, (3, 8), generator=g, device="cuda").half()
+    y = _b().linear(x, w, dtype=torch.float32)
+    assert all(torch.equal(y[:, n], (x.float() * w[n].float()).sum(1)) for n in range(3))      # small whole numbers: exact
