@@ -355,3 +355,25 @@ def test_very_many_rows():
     w = torch.randint(-3, 4, (3, 8), generator=g, device="cuda").half()
     y = _b().linear(x, w, dtype=torch.float32)
     assert all(torch.equal(y[:, n], (x.float() * w[n].float()).sum(1)) for n in range(3))      # small whole numbers: exact
+
+
+@pytest.mark.parametrize("T,N,K,kind", [(290, 11008, 160, "bf16"), (600, 10212, 96, "int8"), (1358, 10211, 264, "f16"),
+                                        (290, 11008, 130, "e4m3"), (4096, 4096, 512, "bf16")])
+def test_linear_over_several_rounds_of_tiles(T, N, K, kind):
+    """Sizes whose tiles do not fill their last round on 148 SMs; every element against 64 bits."""
+    g = torch.Generator().manual_seed(T + N)
+    x, w = (torch.randint(-4, 5, s, generator=g) for s in ((T, K), (N, K)))
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[kind]
+    bias, res = torch.randint(-9, 10, (N,), generator=g).float(), torch.randint(-9, 10, (T, N), generator=g).float()
+    codes = kind in ("int8", "e4m3")
+    xs = 2.0 ** torch.randint(-2, 3, (T,), generator=g) if codes else None
+    ws = 2.0 ** torch.randint(-2, 3, (N,), generator=g) if codes else None
+    pad = torch.zeros(T + N, (K + 15) // 16 * 16)                       # rows on 16 bytes
+    pad[:T, :K], pad[T:, :K] = x, w
+    pad = pad.to(dt).cuda()
+    y = _b().linear(pad[:T, :K], pad[T:, :K], bias.cuda(), residual=res.cuda(), dtype=torch.float32,
+                    x_scale=None if xs is None else xs.cuda(), w_scale=None if ws is None else ws.cuda()).cpu()
+    want = x.double() @ w.double().T
+    if codes:
+        want = want * xs.double()[:, None] * ws.double()[None]
+    assert torch.equal(y.double(), want + bias.double() + res.double())  # whole sixteenths below 2^24: exact
