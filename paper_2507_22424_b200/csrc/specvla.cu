@@ -1360,8 +1360,9 @@ static int finish_verify(specvla_ctx *ctx, const EpArgs &ea, int *accept_len_out
 
 // Validates the call's trees (caller-supplied, or the device-resident ones when trees == NULL),
 // lays the episodes' rows out and uploads caller-supplied trees.
+// want_rows: the rows that the trees must have together, before anything is copied; -1: any.
 static int prepare_trees(specvla_ctx *ctx, int n_ep, const int *episodes, const specvla_tree *trees, EpArgs *ea_out,
-                         int *rows_out, cudaStream_t st) {
+                         int *rows_out, cudaStream_t st, int want_rows = -1) {
   const specvla_model_desc &d = ctx->desc;
   EpArgs ea{};
   ea.n_ep = n_ep;
@@ -1386,6 +1387,7 @@ static int prepare_trees(specvla_ctx *ctx, int n_ep, const int *episodes, const 
     R += rows;
   }
   if (R > d.max_rows || R > ctx->max_lm_rows) return SPECVLA_ERR_CAPACITY;
+  if (want_rows >= 0 && R != want_rows) return SPECVLA_ERR_INVALID_ARG;
   if (trees) {
     DevTree *h = ctx->pin_trees;
     for (int i = 0; i < n_ep; i++) {
@@ -1429,8 +1431,7 @@ int specvla_verify_tree_sampled(specvla_ctx *ctx, int n_ep, const int *episodes,
   int lo, hi;
   argmax_range(ctx, &lo, &hi);
   if (hi - lo > sampled::MAX_IDS) return SPECVLA_ERR_CAPACITY;
-  TRY(prepare_trees(ctx, n_ep, episodes, trees, &ea, &R, st));
-  if (n_rows != R) return SPECVLA_ERR_INVALID_ARG;
+  TRY(prepare_trees(ctx, n_ep, episodes, trees, &ea, &R, st, std::max(n_rows, 0)));
   TRY(verify_device_trees(ctx, ea, R, 0, logits, st, u, temperature));
   return finish_verify(ctx, ea, accept_len_out, tokens_out, st);
 }

@@ -377,3 +377,29 @@ def test_linear_over_several_rounds_of_tiles(T, N, K, kind):
     if codes:
         want = want * xs.double()[:, None] * ws.double()[None]
     assert torch.equal(y.double(), want + bias.double() + res.double())  # whole sixteenths below 2^24: exact
+
+
+def test_context_call_with_another_number_of_rows_leaves_the_drafted_tree(c0, wcuda):
+    import ctypes as C_
+    from paper_2507_22424_b200.binding import Tree, _ints, lib, make_shape
+    host = _tree(5, 1, C.TINY.action_base)
+    results = []
+    for refused in (False, True):
+        gpu = _ctx(c0, wcuda)
+        gpu.prefill([0], c0["embeds"].cuda(), c0["ids"].tolist(), [len(c0["ids"])])
+        n = len(gpu.draft_tree([0], make_shape((2, 2), (1, 2)))[0]["tokens"])
+        u = torch.linspace(0.05, 0.95, n).cuda()
+        if refused:
+            tree = (Tree * 1)()
+            keep = [_ints(host[k]) for k in ("tokens", "parent", "depth")]
+            tree[0].n_rows, tree[0].score = 5, None
+            tree[0].tokens, tree[0].parent, tree[0].depth = keep
+            logits = torch.empty(8, gpu.model.vocab, device="cuda")
+            m, toks = (C_.c_int * 1)(), (C_.c_int * 64)()
+            for rows in (4, 6, 0, -1):
+                assert lib.specvla_verify_tree_sampled(gpu.h, 1, _ints([0]), tree, 1.0, C_.c_void_p(u.data_ptr()),
+                                                       C_.c_void_p(logits.data_ptr()), rows, m, toks, None) == -1
+        results.append(gpu.verify_tree_sampled([0], None, u))
+        gpu.close()
+    (ma, ea, la), (mb, eb, lb) = results
+    assert ma == mb and ea == eb and torch.equal(la, lb)
