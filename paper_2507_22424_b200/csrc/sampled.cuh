@@ -310,7 +310,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) wa
   pdl_launch();
   const DevTree *tr = CTX ? a.trees + ea.eps[seq] : nullptr;
   const long long row0 = CTX ? ea.row0[seq] : (long long)seq * a.rows;
-  const int n = CTX ? tr->n_rows : a.n_rows ? min(max(a.n_rows[seq], 1), a.rows) : a.rows;
+  const int n = CTX ? min(tr->n_rows, ea.nrows[seq]) : a.n_rows ? min(max(a.n_rows[seq], 1), a.rows) : a.rows;
   const int width = a.hi - a.lo;
   auto logits_of = [&](int i) { return static_cast<const T *>(a.logits) + (row0 + i) * a.ld + a.lo; };
   auto probs_of = [&](int i) { return a.probs + (row0 + i) * a.ld_probs + a.lo; };
