@@ -1,0 +1,39 @@
+"""The linear layer's activations over their whole range, relative to the value: arguments come in through the bias, so that
+nothing but the activation and its rounding is left. Bounds: f32 steps are 2^-23, a rounding half of one."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def activated(vals, act, dtype, T):
+    """act(vals) from a product of zeros, by the kernel of few rows (T = 3) or of many (T = 200)."""
+    from paper_2507_22424_b200 import binding as B
+    x, w = torch.zeros(T, 16, dtype=HF, device="cuda"), torch.zeros(len(vals), 16, dtype=HF, device="cuda")
+    y = B.linear(x, w, vals.cuda(), act, dtype=dtype).cpu()
+    assert torch.equal(y, y[:1].expand_as(y))
+    return y[0].double()
+
+
+def arguments(least):
+    v = torch.cat([torch.linspace(least, -least, 4001), torch.logspace(-30, 0, 200), -torch.logspace(-30, 0, 200)])
+    return torch.cat([v, torch.tensor([-4.0, -4.5, -5.0, -5.5, -6.0, 4.0, 6.0])])
+
+
+def gelu(v):
+    """v / 2 erfc(-v / sqrt 2): 1 + erf would cancel in 64 bits too."""
+    return 0.5 * v * torch.erfc(-v * math.sqrt(0.5))
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_gelu_in_f32_keeps_its_tail(T):
+    """Polynomial 1 step and its evaluation 3, reciprocal and exponential 1 and 2, products 2: 9 steps of the tail's own
+    value; 10 are allowed. Down to -13, where the result is 8e-38."""
+    v = arguments(-13.0)
+    want = gelu(v.double())
+    err = (activated(v, "gelu", F32, T) - want).abs()
+    assert (err <= 10 * 2.0 ** -23 * want.abs() + 2.0 ** -149).all(), float((err / want.abs().clamp(min=1e-300)).max())
