@@ -70,15 +70,28 @@ template <bool FAST> __device__ __forceinline__ float sigmoid_times(float v, flo
   }
   return v / (1.f + expf(-z));
 }
-// max(v, 0) - |v| / 2 erfc(|v| / sqrt 2) with erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), off by at
-// most 1.5e-7 (Abramowitz and Stegun 7.1.26; the constants here are a_k / 2 and those for |v| in place of x); negative v
-// take the small product itself, so that nothing cancels. Two at a time: both reciprocals come from the one of their product
-// (the special-function unit takes 8 clocks an instruction). |v| stops at 64, where the product is long 0, so that
+// GELU: max(v, 0) - m / 2 erfc(m / sqrt 2), m = |v|; negative v take the small product itself, so that nothing cancels. It is
+// m p(t) exp(-m^2 / 2), t = 1 / (1 + C m), where p is a polynomial of degree 8 without a constant term, fitted to
+// erfcx(m / sqrt 2) / 2 over 0 <= m <= 14 so that its largest relative error is smallest (9e-8; Lawson's reweighted least
+// squares): right relative to itself, as far down as it is a number. |v| stops at 64, where the product is long 0, so that
 // everything stays in range, and 0 v keeps the NaN of a NaN and of -infinity. No branch on v: 15 us instead of 11 for
 // 1001 x 4331 x 128.
+constexpr float GELU_C = 0.304595530f;
+__device__ __forceinline__ float gelu_poly(float t) {
+  float p = fmaf(t, 0.0367648005f, -0.153923899f);
+  p = fmaf(p, t, 0.188323691f);
+  p = fmaf(p, t, -0.0400405787f);
+  p = fmaf(p, t, 0.122031376f);
+  p = fmaf(p, t, 0.10302265f);
+  p = fmaf(p, t, 0.122346029f);
+  return fmaf(p, t, 0.12147598f) * t;
+}
+// For 16-bit results, two at a time: both reciprocals come from the one of their product (the special-function unit takes 8
+// clocks an instruction), and the exponent keeps its roundings (a product off by 1.5e-6 of itself at most, and 3 * 2^-24 m^2 / 2 more:
+// 2e-6 where f16 ends, 1e-5 at -13).
 __device__ __forceinline__ void fast_gelu(float &v0, float &v1) {
   const float m[2] = {fminf(fabsf(v0), 64.f), fminf(fabsf(v1), 64.f)};
-  const float d0 = fmaf(0.23164189f, m[0], 1.f), d1 = fmaf(0.23164189f, m[1], 1.f);
+  const float d0 = fmaf(GELU_C, m[0], 1.f), d1 = fmaf(GELU_C, m[1], 1.f);
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
   const float t[2] = {r * d1, r * d0};
@@ -87,37 +100,23 @@ __device__ __forceinline__ void fast_gelu(float &v0, float &v1) {
     float &v = k ? v1 : v0;
     float e;
     asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-0.72134752f * m[k] * m[k]));
-    float p = fmaf(t[k], 0.5307027145f, -0.7265760135f);
-    p = fmaf(p, t[k], 0.7107068705f);
-    p = fmaf(p, t[k], -0.142248368f);
-    p = fmaf(p, t[k], 0.127414796f) * t[k];
     const float flat = 0.f * v, base = v > 0.f ? v : flat;
-    v = fmaf(-m[k], p * e, base);
+    v = fmaf(-(gelu_poly(t[k]) * m[k]), e, base);
   }
 }
-// The same sum for fp32 results: m / 2 erfc(m / sqrt 2) = m p(t) exp(-m^2 / 2), t = 1 / (1 + c m), where p is a polynomial of degree 8
-// without a constant term, fitted to erfcx(m / sqrt 2) / 2 over 0 <= m <= 14 so that its largest relative error is
-// smallest (9e-8; Lawson's reweighted least squares), and the roundings of m^2 and of the exponent are put back: the small
-// product is right to ten 2^-23 of itself at worst, as far down as it is a number. (v / 2 (1 + erf) cancels below -2: 4 % off
-// at -5, and 0 from -5.6 on.)
+// For fp32 results the roundings of m^2 and of the exponent are put back: the product is right to ten 2^-23 of itself at
+// worst. (v / 2 (1 + erf) cancels below -2: 4 % off at -5, and 0 from -5.6 on.)
 __device__ __forceinline__ float exact_gelu(float v) {
   const float m = fminf(fabsf(v), 64.f);
   float t, e;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(t) : "f"(fmaf(0.304595530f, m, 1.f)));
-  float p = fmaf(t, 0.0367648005f, -0.153923899f);
-  p = fmaf(p, t, 0.188323691f);
-  p = fmaf(p, t, -0.0400405787f);
-  p = fmaf(p, t, 0.122031376f);
-  p = fmaf(p, t, 0.10302265f);
-  p = fmaf(p, t, 0.122346029f);
-  p = fmaf(p, t, 0.12147598f) * t;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(t) : "f"(fmaf(GELU_C, m, 1.f)));
   constexpr float H = 0.7213475108f, HL = 9.6298e-9f;        // log2(e) / 2 = H + HL
   const float sq = m * m, y = H * sq;
   const float lost = fmaf(HL, sq, fmaf(H, fmaf(m, m, -sq), fmaf(H, sq, -y)));
   asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-y));
   e = fmaf(e, -0.693147181f * lost, e);
   const float flat = 0.f * v, base = v > 0.f ? v : flat;
-  return fmaf(-(p * m), e, base);
+  return fmaf(-(gelu_poly(t) * m), e, base);
 }
 template <bool FAST, int M> __device__ __forceinline__ void activate(float (&v)[M], int act) {
   switch (act) {

@@ -37,3 +37,17 @@ def test_gelu_in_f32_keeps_its_tail(T):
     want = gelu(v.double())
     err = (activated(v, "gelu", F32, T) - want).abs()
     assert (err <= 10 * 2.0 ** -23 * want.abs() + 2.0 ** -149).all(), float((err / want.abs().clamp(min=1e-300)).max())
+
+
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_gelu_in_16_bits_is_off_by_its_rounding(dtype, T):
+    """Before the result's own half step: polynomial, reciprocals, exponential and products as above, 12 * 2^-23 in all; three
+    roundings of the exponent v^2 / 2, each 2^-24 of it. Below half a step of f16 (2^-25) nothing but the rounding counts."""
+    v = arguments(-13.0)
+    want = gelu(v.double())
+    least = 2.0 ** -25 if dtype == HF else 2.0 ** -134
+    before = 12 * 2.0 ** -23 + 3 * 2.0 ** -24 * v.double() ** 2 / 2
+    err = (activated(v, "gelu", dtype, T) - want).abs()
+    tol = (before + torch.finfo(dtype).eps / 2 * (1 + before)) * want.abs() + least
+    assert (err <= tol).all(), float((err / want.abs().clamp(min=1e-300))[want.abs() > 1e-4].max())
