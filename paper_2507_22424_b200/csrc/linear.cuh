@@ -59,16 +59,19 @@ __device__ __forceinline__ void put2(float *p, float a, float b) { *reinterpret_
 __device__ __forceinline__ void put2(bf16 *p, float a, float b) { *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b); }
 __device__ __forceinline__ void put2(__half *p, float a, float b) { *reinterpret_cast<__half2 *>(p) = __floats2half2_rn(a, b); }
 
-// FAST: for results that are rounded to 16 bits. exp2 and the reciprocal of the special-function unit (2^-22 relative)
-// in place of expf and a division; tanh through v / (1 + exp(-2z)), which cancels nothing.
+// v / (1 + exp(-z)) through exp(-|z|), which never overflows: small results are numbers as long as exp is one. FAST: for results
+// that are rounded to 16 bits, exp2 and the reciprocal of the special-function unit (2^-22 relative) in place of expf and a
+// division. tanh goes through this sum too, which cancels nothing.
 template <bool FAST> __device__ __forceinline__ float sigmoid_times(float v, float z) {
+  float e;
   if (FAST) {
-    float e, r;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-1.442695041f * z));
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-1.442695041f * fabsf(z)));
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    return v * r;
+    return (z < 0.f ? v * e : v) * r;
   }
-  return v / (1.f + expf(-z));
+  e = expf(-fabsf(z));
+  return (z < 0.f ? v * e : v) / (1.f + e);
 }
 // GELU: max(v, 0) - m / 2 erfc(m / sqrt 2), m = |v|; negative v take the small product itself, so that nothing cancels. It is
 // m p(t) exp(-m^2 / 2), t = 1 / (1 + C m), where p is a polynomial of degree 8 without a constant term, fitted to

@@ -51,3 +51,30 @@ def test_gelu_in_16_bits_is_off_by_its_rounding(dtype, T):
     err = (activated(v, "gelu", dtype, T) - want).abs()
     tol = (before + torch.finfo(dtype).eps / 2 * (1 + before)) * want.abs() + least
     assert (err <= tol).all(), float((err / want.abs().clamp(min=1e-300))[want.abs() > 1e-4].max())
+
+
+def silu(v):
+    return v * torch.sigmoid(v)
+
+
+def gelu_tanh(v):
+    """v / 2 (1 + tanh z) = v sigmoid(2 z)"""
+    return v * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3))
+
+
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("act,least", [("silu", -103.0), ("gelu_tanh", -10.7)])
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+def test_sigmoids_keep_their_tail(dtype, act, least, T):
+    """exp(-z), z the sigmoid's argument: five roundings of z (SiLU: one) and the constant's, 2^-24 each of |z|, the exponential
+    2^-22, the reciprocal (or the division) and products 2^-22; then half a step. As far as exp(-|z|) is a number, which below 2^-126 is
+    one in steps of 2^-149 that the factor v scales."""
+    v = arguments(least)
+    f = silu if act == "silu" else gelu_tanh
+    want = f(v.double())
+    z = v.double().abs() if act == "silu" else 2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v.double() ** 3).abs()
+    before = 2.0 ** -20 + 6 * 2.0 ** -24 * z
+    err = (activated(v, act, dtype, T) - want).abs()
+    small = {F32: 2.0 ** -149, BF: 2.0 ** -134, HF: 2.0 ** -25}[dtype] + 2.0 ** -149 * v.abs().double()
+    tol = (before + torch.finfo(dtype).eps / 2 * (1 + before)) * want.abs() + small
+    assert (err <= tol).all(), v[err > tol]
