@@ -214,7 +214,7 @@ struct Walk {
   int tok[SV_MAX_TREE];
   int inner[SV_MAX_TREE];                 // the row has children
   alignas(16) int parent[SV_MAX_TREE];    // -1 past the last row
-  int yes[SV_MAX_TREE];                   // no PROBS: the row is accepted if the walk comes to it
+  int yes[SV_MAX_TREE];                   // no PROBS: the row is accepted if the walk comes to it; 2: not yet decided
   int again[SV_MAX_TREE];                 // no PROBS: an elder sibling has the same token
   int path[SV_MAX_TREE];
   int refused[SV_MAX_TREE];               // tokens refused at the row where the walk ends, each once
@@ -222,7 +222,46 @@ struct Walk {
   double beta, S;
   double part[2][CLUSTER * WALK_THREADS / 32];   // sums of the cluster's warps, by turns
   float part_max[2][CLUSTER * WALK_THREADS / 32];
+  double left[WALK_THREADS / 32];
 };
+
+// The children that put_yes left open (of row `of`, or of all rows where it is -1), from the sums of their parents' rows without
+// the tokens refused before them (whole CTA). z0: the tree's first row.
+template <typename T>
+static __device__ __noinline__ void settle_yes(Walk &w, const ExpTable &tab, const T *z0, long long ld, int n, int width, int n_sub,
+                                               float temperature, double factor, int of) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int j = 1; j < n; j++) {
+    const int i = w.parent[j];
+    if (i < 0 || (of >= 0 && i != of) || w.yes[j] != 2) continue;
+    const T *z1 = z0 + i * ld;
+    const RowExp weight(w.zmax[i], temperature, factor);
+    double s = 0.0;
+    for (int k = warp; k < n_sub; k += WALK_THREADS / 32) {
+      float z[16];
+      load_piece<false>(z1, k * SUB, width, aligned4(z1), z);
+      uint32_t out = 0;                                          // this lane's refused ones
+      for (int r = i + 1; r < j; r++) {
+        const int at = w.parent[r] == i ? w.tok[r] - k * SUB : -1;
+        if (at >= 0 && at < SUB && (at >> 2 & 31) == lane) out |= 1u << (at >> 7 << 2 | (at & 3));
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const double v = weight(z[e], tab);                      // (past the last id: -inf)
+        s += out >> e & 1 ? 0.0 : v;
+      }
+    }
+    s = warp_sum64(s);
+    if (lane == 0) w.left[warp] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      double S = 0.0;
+      for (int k = 0; k < WALK_THREADS / 32; k++) S += w.left[k];
+      w.yes[j] = (double)w.u[j] * S < w.w[j];
+    }
+    __syncthreads();
+  }
+}
 
 // The piece at `target` of n sums (whole warp), and the cumulative sum before it; the last piece that has any weight
 // where none reaches it, -1: none has.
@@ -383,20 +422,30 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) wa
     const double v = inside ? weight_of(my_parent, my_z, my_x) : 0.0;
     w.w[tid] = PROBS ? (inside ? v / sum_of(my_parent) : 0.0) : v;
   };
-  // no PROBS: whether the thread's row is accepted if the walk comes to it; S: what is left of the parent's row then
+  // no PROBS: whether the thread's row is accepted if the walk comes to it; S: what is left of the parent's row then. The
+  // subtraction leaves an error of up to 2^-40 of the whole in S (the weights' 4e-14 each, roundings); where that could turn the
+  // decision, S is summed without the refused tokens (settle_yes). true: that is to be done.
   auto put_yes = [&]() {
-    bool yes = false;
-    if (inside && !w.again[tid]) {
-      double S = sum_of(my_parent);
+    int yes = 0;
+    if (inside && !w.again[tid] && w.w[tid] > 0.0) {
+      const double whole = sum_of(my_parent), u = w.u[tid];
+      double S = whole;
 #pragma unroll
       for (int k = 0; k < 4; k++)
         for (uint32_t left = elder[k]; left; left &= left - 1) {
           const int j = 32 * k + __ffs(left) - 1;
           if (!w.again[j]) S -= w.w[j];
         }
-      yes = w.w[tid] > 0.0 && (double)w.u[tid] * S < w.w[tid];
+      const double off = S < whole ? 0x1p-40 * whole : 0.0;
+      yes = u * (S + off) < w.w[tid] ? 1 : u * (S - off) < w.w[tid] ? 2 : 0;
     }
     w.yes[tid] = yes;
+    return yes == 2;
+  };
+  auto decide = [&](bool mine, int of) {
+    const bool open = mine && put_yes();
+    if (__syncthreads_or(open))
+      settle_yes(w, tab, logits_of(0), a.ld, n, width, a.n_sub, a.temperature, a.factor, of);
   };
   if (tid < n) {
     w.q[tid] = my_q;
@@ -424,8 +473,7 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) wa
   }
   __syncthreads();
   if (!PROBS && !LAZY) {                                         // every child is decided at once
-    if (tid < n) put_yes();
-    __syncthreads();
+    decide(tid < n, -1);
   }
   if (CLUSTERED) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
@@ -476,11 +524,8 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) wa
         if (tid == 0) w.zmax[cur] = M, w.z[cur] = S;
         __syncthreads();
         if (tid < n && my_parent == cur) put_weight();
-        if (!PROBS) {
-          __syncthreads();
-          if (tid < n && my_parent == cur) put_yes();
-        }
         __syncthreads();
+        if (!PROBS) decide(tid < n && my_parent == cur, cur);
       }
     }
     if (warp == 0) {

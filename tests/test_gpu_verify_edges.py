@@ -1,0 +1,54 @@
+"""Verification by random numbers where it can go wrong: against the 64-bit definition (operator_refs.py)."""
+import numpy as np
+import pytest
+import torch
+
+import operator_refs as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def _b():
+    from paper_2507_22424_b200 import binding
+    return binding
+
+
+def check(logits, tokens, parent, u, **kw):
+    cu = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+    got = _b().verify_sampled(logits.cuda(), tokens.cuda(), parent.cuda(), u.cuda(), **cu)
+    want = ref.verify_sampled(logits, tokens, parent, u, **kw)
+    for a, b in zip(got, want):
+        assert torch.equal(a.cpu(), b), (a.cpu()[(a.cpu() != b).view(len(b), -1).any(1)], b[(a.cpu() != b).view(len(b), -1).any(1)])
+    return want
+
+
+@pytest.mark.parametrize("rows", [4, 60])
+@pytest.mark.parametrize("vocab", [40, 700])
+def test_little_is_left_after_refused_tokens(rows, vocab):
+    """Two siblings with nearly all of the weight are refused; the third is decided by a random number 2^-20 beside its share of
+    what is left (1e-14 of the row): what is left has to be right relative to itself. rows = 60: summed as the walk comes to them."""
+    n = 400 if rows == 60 else 64
+    g = torch.Generator().manual_seed(vocab)
+    logits = torch.full((n, rows, vocab), -60.0)
+    logits[:, 0, 3] = 0.0
+    logits[:, 0, vocab - 2] = -16.0 - torch.rand(n, generator=g)
+    logits[:, 0, 7] = logits[:, 0, vocab - 2] - 16.0 - torch.rand(n, generator=g)
+    logits[:, 0, vocab // 2] = logits[:, 0, 7] + torch.randn(n, generator=g)
+    parent = torch.full((n, rows), -1, dtype=torch.int32)
+    parent[:, 1:4] = 0
+    tokens = torch.zeros(n, rows, dtype=torch.int32)
+    tokens[:, 1], tokens[:, 2], tokens[:, 3] = 3, vocab - 2, 7
+    u = torch.rand(n, rows, generator=g)
+    u[:, 1] = u[:, 2] = 1 - 2.0 ** -24
+    w = torch.exp(logits[:, 0].double())
+    left = w.clone()
+    left[:, 3] = left[:, vocab - 2] = 0
+    share = w[:, 7] / left.sum(1)
+    up = torch.arange(n) % 2 == 1
+    u[:, 3] = (share * torch.where(up, 1 + 2.0 ** -20, 1 - 2.0 ** -20)).float()
+    m = check(logits, tokens, parent, u)[0]
+    # (a first token with more than 1 - 2^-24 of the weight is accepted)
+    third = (w[:, 3] / w.sum(1) <= u[:, 1].double()) & (w[:, vocab - 2] / (w.sum(1) - w[:, 3]) <= u[:, 2].double())
+    assert torch.equal(m[third], (~up).int()[third]) and third.sum() > n // 4
