@@ -594,9 +594,10 @@ def linear_status():
 
 def _row_distance(t, name, n, rows, vocab):
     s = t.stride()
-    if t.shape != (n, rows, vocab) or s[2] != 1 or (n > 1 and s[0] != rows * s[1]) or (n * rows > 1 and s[1] < vocab):
+    ld = s[1] if rows > 1 else s[0]                                  # (a dimension of one has no distance)
+    if t.shape != (n, rows, vocab) or (vocab > 1 and s[2] != 1) or (n > 1 and rows > 1 and s[0] != rows * ld) or (n * rows > 1 and ld < vocab):
         raise ValueError(f"{name} must be {(n, rows, vocab)} with rows at one distance")
-    return s[1] if s[1] > vocab else vocab
+    return ld if ld > vocab else vocab
 
 
 def _whole(t, name, dtype, shape):

@@ -52,3 +52,39 @@ def test_little_is_left_after_refused_tokens(rows, vocab):
     # (a first token with more than 1 - 2^-24 of the weight is accepted)
     third = (w[:, 3] / w.sum(1) <= u[:, 1].double()) & (w[:, vocab - 2] / (w.sum(1) - w[:, 3]) <= u[:, 2].double())
     assert torch.equal(m[third], (~up).int()[third]) and third.sum() > n // 4
+
+
+@pytest.mark.parametrize("with_probs", [False, True])
+@pytest.mark.parametrize("kind", [F32, BF])
+def test_trees_of_one_row_at_any_distance(kind, with_probs):
+    """The last row of every sequence's logits, padded rows with a dimension of one between, and ids of one: a distance of a
+    dimension of one is no distance."""
+    g = torch.Generator().manual_seed(5)
+    n, vocab = 7, 300
+    wide = (torch.randn(n, 4, vocab + 20, generator=g) * 3).to(kind)
+    probs = torch.softmax(torch.randn(n, 3, vocab + 4, generator=g), -1)
+    tokens, parent = torch.zeros(n, 1, dtype=torch.int32), torch.full((n, 1), -1, dtype=torch.int32)
+    u = torch.rand(n, 1, generator=g)
+    z, q = wide[:, -1:, :vocab], probs[:, 1:2, :vocab] if with_probs else None
+    want = ref.verify_sampled(z, tokens, parent, u, draft_probs=q)
+    cw, cp = wide.cuda(), probs.cuda()
+    for zc in (cw[:, -1:, :vocab], cw[:, -1].unsqueeze(1)[..., :vocab], cw.as_strided((n, 1, vocab), (4 * (vocab + 20), 3, 1), 3 * (vocab + 20))):
+        got = _b().verify_sampled(zc, tokens.cuda(), parent.cuda(), u.cuda(), draft_probs=cp[:, 1:2, :vocab] if with_probs else None)
+        for a, b in zip(got, want):
+            assert torch.equal(a.cpu(), b)
+    one = cw[:, :, 5:6]                                              # a vocabulary of one id
+    tokens, parent = torch.zeros(n, 4, dtype=torch.int32), torch.tensor([[-1, 0, 1, 2]], dtype=torch.int32).repeat(n, 1)
+    u = torch.rand(n, 4, generator=g)
+    want = ref.verify_sampled(wide[:, :, 5:6], tokens, parent, u)
+    for zc in (one, one.contiguous(), one.contiguous().as_strided((n, 4, 1), (4, 1, 9))):
+        got = _b().verify_sampled(zc, tokens.cuda(), parent.cuda(), u.cuda())
+        for a, b in zip(got, want):
+            assert torch.equal(a.cpu(), b)
+
+
+def test_rows_that_overlap_are_refused():
+    z = torch.zeros(40, device="cuda")
+    i, u = torch.zeros(3, 1, dtype=torch.int32, device="cuda"), torch.zeros(3, 1, device="cuda")
+    for zc in (z.as_strided((3, 1, 10), (9, 1, 1)), z.as_strided((3, 1, 10), (0, 10, 1)), z.as_strided((3, 1, 10), (10, 10, 2))):
+        with pytest.raises(ValueError):
+            _b().verify_sampled(zc, i, i, u)
