@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import threading
 
 import torch
 
@@ -440,6 +441,7 @@ ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 _FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
 _CODES = frozenset((torch.int8, torch.float8_e4m3fn))
 _status_words = {}
+_status_lock = threading.Lock()
 
 
 def _device(*tensors):
@@ -537,8 +539,12 @@ def _status_word(dev):
     if word is None:
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("the first linear() on a device must not be inside a stream capture")
-        word = _status_words[dev] = torch.zeros(1, dtype=torch.int32, device="cuda")
-        torch.cuda.synchronize()
+        with _status_lock:                                           # (of several threads' first calls one makes it)
+            word = _status_words.get(dev)
+            if word is None:
+                word = torch.zeros(1, dtype=torch.int32, device="cuda")
+                torch.cuda.synchronize()
+                _status_words[dev] = word
     return word
 
 
