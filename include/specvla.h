@@ -395,8 +395,9 @@ int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ld
  * start on 16 bytes (base address and ld); Y and residual on their own element. Y may be the residual itself. Values
  * that are not finite reach what depends on them only.
  * status: one word, zeroed by the caller before its first use and left alone by calls that succeed: a bounded
- * device-side wait that gave up sets it, and specvla_gemm_status(status, stream) then reports
- * SPECVLA_ERR_TIMEOUT (Y is undefined; zero the word to use it again). */
+ * device-side wait that gave up adds to it, and specvla_gemm_status(status, stream) then reports
+ * SPECVLA_ERR_TIMEOUT (Y is undefined). Zero the word to use it again, when no call that has it is in flight: calls that share
+ * a word cannot tell whose wait it was. */
 #define SPECVLA_ACT_NONE      0
 #define SPECVLA_ACT_RELU      1
 #define SPECVLA_ACT_GELU      2   /* v / 2 (1 + erf(v / sqrt 2)) */

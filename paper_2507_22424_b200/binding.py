@@ -440,8 +440,20 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, t
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 _FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
 _CODES = frozenset((torch.int8, torch.float8_e4m3fn))
-_status_words = {}
+
+
+class _Seen(threading.local):
+    """Per device, how many waits that gave up this host thread has been told of."""
+
+    def __init__(self):
+        self.count = {}
+
+
+# Kernels add to a device's word when a wait gives up, and nobody takes anything from it: so no thread or stream can clear
+# what another's call is about to report.
+_status_words, _status_told, _status_seen = {}, {}, _Seen()
 _status_lock = threading.Lock()
+ERR_TIMEOUT = -6
 
 
 def _device(*tensors):
@@ -545,6 +557,8 @@ def _status_word(dev):
                 word = torch.zeros(1, dtype=torch.int32, device="cuda")
                 torch.cuda.synchronize()
                 _status_words[dev] = word
+    if dev not in _status_seen.count:
+        _status_seen.count[dev] = _status_told.get(dev, 0)           # (what has been told before is no news)
     return word
 
 
@@ -589,12 +603,19 @@ def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=Non
 
 
 def linear_status():
-    """Synchronises the current stream; raises SpecVLAError(-6) if a linear() call on this device gave up since the
-    last time (its result is undefined), and clears the status."""
-    word = _status_word(_device())
+    """Synchronises the current stream; raises SpecVLAError(-6) if a linear() call on this device gave up since the last
+    time (its result is undefined). Every host thread that has called linear() on the device is told once, whichever
+    thread's or stream's call it was."""
+    dev = _device()
+    word = _status_word(dev)
     rc = lib.specvla_gemm_status(C.c_void_p(word.data_ptr()), _stream())
-    if rc != 0:
-        word.zero_()
+    if rc == ERR_TIMEOUT:
+        count = int(word.item())
+        if count == _status_seen.count[dev]:
+            return
+        with _status_lock:
+            _status_told[dev] = max(count, _status_told.get(dev, 0))
+        _status_seen.count[dev] = count
     _run(rc)
 
 

@@ -30,10 +30,6 @@ constexpr int RING = 208 * 1024;
 constexpr int SMEM = RING + 1024;
 constexpr int THREADS = 192;               // warp 0 copies, warp 1 MMAs, warps 2-5 epilogue
 
-#define SV_ERR_LINEAR_EMPTY 11
-#define SV_ERR_LINEAR_FULL 12
-#define SV_ERR_LINEAR_ACC 13
-
 struct Args {
   int T, N, KB;                            // K blocks
   int tn;                                  // rows per chunk = rows of an X box, a multiple of 16
@@ -46,7 +42,7 @@ struct Args {
   long long ldr, ldy;
   unsigned long long wait_ns;
   int withhold;                            // test hook: > 0: the K block (withhold - 1) of every CTA is never loaded
-  int *status;
+  int *status;                             // waits that gave up add to it
 };
 
 __device__ __forceinline__ float as_float(float v) { return v; }
@@ -334,8 +330,8 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const long long row0 = (long long)chunk * a.tn;
   const int T = min(a.T - chunk * a.tn, a.tn);
   const int cols = tmem_cols(a.tn);
-  auto fail = [&](int code) {
-    atomicExch(a.status, code);
+  auto fail = [&]() {
+    atomicAdd(a.status, 1);
     s_fail = 1;
   };
   if (threadIdx.x == 0) {
@@ -368,7 +364,7 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     for (int it = 0, st = 0, ph = 1; it < n_kb; it++) {
       const bool ok = mbar_wait(empty_bar(st), ph, a.wait_ns);
       if (!__all_sync(0xffffffffu, ok)) {
-        if (lead) fail(SV_ERR_LINEAR_EMPTY);
+        if (lead) fail();
         break;
       }
       if (lead && it != a.withhold - 1) {
@@ -389,7 +385,7 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     for (int it = 0, st = 0, ph = 0; it < n_kb; it++) {
       const bool ok = mbar_wait(full_bar(st), ph, a.wait_ns);
       if (!__all_sync(0xffffffffu, ok)) {
-        if (lead) fail(SV_ERR_LINEAR_FULL);
+        if (lead) fail();
         break;
       }
       tc_fence_after();
@@ -416,7 +412,7 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     if (et == 0) {                                             // one thread polls, the others sleep
       const bool ok = mbar_wait(acc_bar, 0, a.wait_ns);
       s_done = ok;
-      if (!ok) fail(SV_ERR_LINEAR_ACC);
+      if (!ok) fail();
     }
     asm volatile("bar.sync 1, 128;" ::: "memory");
     tc_fence_after();
@@ -602,8 +598,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
   const int total = p.tiles * p.chunks;
   // a wait that gave up: both CTAs of the pair leave in the same way
-  auto fail = [&](int code) {
-    atomicExch(a.status, code);
+  auto fail = [&]() {
+    atomicAdd(a.status, 1);
     for (uint32_t r = 0; r < 2; r++)
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(&s_fail), r)), "r"(1) : "memory");
   };
@@ -647,7 +643,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       for (int kb = 0; kb < a.KB; kb++, n++) {
         ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(st), ph, a.wait_ns));
         if (!ok) {
-          if (lead) fail(SV_ERR_LINEAR_EMPTY);
+          if (lead) fail();
           break;
         }
         if (lead && n != a.withhold - 1) {
@@ -672,7 +668,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       for (int i = pair; ok && i < total; i += pairs) {
         ok = __all_sync(0xffffffffu, mbar_wait(free_bar(buf), fph, a.wait_ns));
         if (!ok) {
-          if (lead) fail(SV_ERR_LINEAR_ACC);
+          if (lead) fail();
           break;
         }
         tc_fence_after();
@@ -680,7 +676,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         for (int kb = 0; kb < a.KB; kb++) {
           ok = __all_sync(0xffffffffu, mbar_wait(full_bar(st), ph, a.wait_ns));
           if (!ok) {
-            if (lead) fail(SV_ERR_LINEAR_FULL);
+            if (lead) fail();
             break;
           }
           tc_fence_after();
@@ -718,7 +714,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       if (et == 0) {
         const bool ok = mbar_wait(acc_bar(buf), ph, a.wait_ns);
         s_done[buf] = ok;
-        if (!ok) fail(SV_ERR_LINEAR_ACC);
+        if (!ok) fail();
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (!s_done[buf]) break;
