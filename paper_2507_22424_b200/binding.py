@@ -562,10 +562,15 @@ def _status_word(dev):
     return word
 
 
+def _not_on_16(name, address, ld, step):
+    raise ValueError(f"{name}: rows must start on 16 bytes (address {address:#x}, rows {ld * step} bytes apart)")
+
+
 def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=None, dtype=None, out=None):
     """specvla_linear: act(x @ w.T * scales + bias) + residual. x [T, K] and w [N, K] of one type (bf16, f16, int8,
     float8_e4m3fn), scales f32 [T] and [N] with the 8-bit ones, bias f32 [N]; dtype: of the result and the residual
     (default: x's, bf16 for 8-bit operands). out: where the result goes, the residual itself is allowed.
+    Rows of x and w start on 16 bytes (an address and a row distance: pad rows of other lengths and pass a view).
     Asynchronous: linear_status() reports a device-side wait that gave up."""
     T, K = _matrix(x, "x")
     N = _matrix(w, "w")[0]
@@ -575,6 +580,11 @@ def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=Non
         raise ValueError(f"x has type {kind}")
     same = (kind,)
     ldx, ldw = _rows(x, "x", T, K, same), _rows(w, "w", N, K, same)
+    xp, wp, step = x.data_ptr(), w.data_ptr(), 1 if codes else 2
+    if (xp | (ldx * step if T > 1 else 0)) & 15:
+        _not_on_16("x", xp, ldx, step)
+    if (wp | (ldw * step if N > 1 else 0)) & 15:
+        _not_on_16("w", wp, ldw, step)
     if dtype is None:
         dtype = out.dtype if out is not None else torch.bfloat16 if codes else kind
     if dtype not in _FLOATS:
@@ -596,7 +606,7 @@ def linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=Non
         if not K:
             raise ValueError("K is 0")
         _run(lib.specvla_linear(
-            LINEAR_ARGS.pack(T, N, K, TYPES[kind], TYPES[dtype], ACTS[act], x.data_ptr(), ldx, xs_p, w.data_ptr(), ldw, ws_p,
+            LINEAR_ARGS.pack(T, N, K, TYPES[kind], TYPES[dtype], ACTS[act], xp, ldx, xs_p, wp, ldw, ws_p,
                              bias_p, res_p, ldr, y.data_ptr(), ldy, _status_word(dev).data_ptr()),
             torch._C._cuda_getCurrentRawStream(dev)))
     return y

@@ -114,3 +114,15 @@ def test_binding_refuses_host_tensors_and_shapes(B):
                  lambda: B.verify_sampled(x, x, x, x), lambda: B.verify_sampled(x[None], x[None].int()[..., 0], x[None].int()[..., 0], x[:1, :3])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("kind,k,step", [("bfloat16", 5, 8), ("float16", 12, 8), ("int8", 24, 16), ("float8_e4m3fn", 8, 16)])
+def test_binding_names_operands_whose_rows_do_not_start_on_16_bytes(B, kind, k, step):
+    import torch
+    kind = getattr(torch, kind)
+    good = torch.zeros(6, step * 4).to(kind)[:, :k]
+    for x, w, name in ((torch.zeros(6, k).to(kind), good, "x"), (good, torch.zeros(6, k).to(kind), "w"),
+                       (torch.zeros(6, step * 4 + 1).to(kind)[:, :k], good, "x"), (torch.zeros(6, step * 4).to(kind)[:, 1:k + 1], good, "x"),
+                       (good, torch.zeros(6 * step * 4 + 1).to(kind)[1:].view(6, step * 4)[:, :k], "w")):
+        with pytest.raises(ValueError, match=f"{name}.*16 bytes"):
+            B.linear(x, w)
