@@ -309,8 +309,12 @@ int specvla_verify_sampled(const specvla_verify_args *v, void *scratch, size_t s
   a.out_m = v->accept_len, a.out_tok = v->tokens_out, a.out_path = v->path;
   a.out_width = v->rows;
   const EpArgs none = {};
-  return sampled::enqueue<false>(a, none, v->logits_type == SPECVLA_F32 ? 0 : v->logits_type == SPECVLA_BF16 ? 1 : 2, v->n_seq,
-                                 v->n_seq * v->rows, static_cast<cudaStream_t>(stream)) == cudaSuccess
-             ? SPECVLA_OK
-             : (cudaGetLastError(), SPECVLA_ERR_CUDA);
+  const int total = v->n_seq * v->rows;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t err = v->logits_type == SPECVLA_F32    ? sampled::enqueue<float, false>(a, none, v->n_seq, total, st)
+                          : v->logits_type == SPECVLA_BF16 ? sampled::enqueue<bf16, false>(a, none, v->n_seq, total, st)
+                                                           : sampled::enqueue<__half, false>(a, none, v->n_seq, total, st);
+  if (err == cudaSuccess) return SPECVLA_OK;
+  cudaGetLastError();
+  return SPECVLA_ERR_CUDA;
 }

@@ -177,8 +177,7 @@ __device__ __forceinline__ void sum_piece(const Args &a, const T *z0, int sub, i
   s = warp_sum64(s);
 }
 
-// CTX: row numbers of a context's call (no rows are left out). A CTA takes a.per_cta pieces of one row, its warps in turn;
-// a warp asks for its next piece before it sums the present one.
+// CTX: row numbers of a context's call (no rows are left out). A CTA takes a.per_cta pieces of one row, its warps in turn.
 template <typename T, bool CTX>
 static __global__ void __launch_bounds__(STATS_THREADS, 6) stats_kernel(const Args a) {
   __shared__ ExpTable tab;
@@ -760,9 +759,9 @@ static __global__ void __launch_bounds__(WALK_THREADS, PROBS || LAZY ? 2 : 1) wa
   }
 }
 
-// Both launches; type: of the logits (f32, bf16, f16). A context's call has its rows in ea and its trees in a.trees.
+// Both launches. CTX: a context's call, which has its rows in ea and its trees in a.trees.
 template <typename T, bool CTX>
-inline cudaError_t enqueue_t(Args a, const EpArgs &ea, int n_seq, int total_rows, cudaStream_t st) {
+inline cudaError_t enqueue(Args a, const EpArgs &ea, int n_seq, int total_rows, cudaStream_t st) {
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -806,17 +805,11 @@ inline cudaError_t enqueue_t(Args a, const EpArgs &ea, int n_seq, int total_rows
       return err;
     return cudaLaunchKernelEx(&cfg, kernel, a, ea);
   };
-  if constexpr (!CTX) {
+  if constexpr (CTX) {                                           // (a context has no draft probabilities)
+    return go(walk_kernel<T, false, false, true>);
+  } else {
     if (lazy) return a.probs ? go(walk_kernel<T, true, true, false>) : go(walk_kernel<T, false, true, false>);
-  }
-  return a.probs ? go(walk_kernel<T, true, false, CTX>) : go(walk_kernel<T, false, false, CTX>);
-}
-template <bool CTX>
-inline cudaError_t enqueue(const Args &a, const EpArgs &ea, int type, int n_seq, int total_rows, cudaStream_t st) {
-  switch (type) {
-    case 0: return enqueue_t<float, CTX>(a, ea, n_seq, total_rows, st);
-    case 1: return enqueue_t<bf16, CTX>(a, ea, n_seq, total_rows, st);
-    default: return enqueue_t<__half, CTX>(a, ea, n_seq, total_rows, st);
+    return a.probs ? go(walk_kernel<T, true, false, false>) : go(walk_kernel<T, false, false, false>);
   }
 }
 

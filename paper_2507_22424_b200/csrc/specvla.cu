@@ -1317,7 +1317,7 @@ static int verify_device_trees(specvla_ctx *ctx, const EpArgs &ea, int R, int r,
     a.out_tok = ctx->out_tok;
     a.out_path = ctx->out_path;
     a.out_width = SV_MAX_DEPTH + 1;
-    CU(sampled::enqueue<true>(a, ea, 0, n_ep, R, st));
+    CU((sampled::enqueue<float, true>(a, ea, n_ep, R, st)));
     ctx->launches += 2;
     LAUNCH(tree::commit_path_kernel, dim3(n_ep), dim3(128), ea, ctx->st, (const float *)ctx->x, ctx->last_ssq, ctx->last_nt,
            ctx->final_norm, d.rms_eps, d.d_model, ctx->pend_feat, (const int *)ctx->out_m, (const int *)ctx->out_tok,
