@@ -148,9 +148,12 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   double cost = rounds * (((KB + p.S - 1) / p.S) * (256. + 2 * p.tn) + 8000 + 24 * p.tn);
   if (p.S > 1) cost += 2500 + (p.tn / (8 * p.S) + 1) * 1000;
   cost = std::max(cost, read);
-  if (rounds > 1) cost *= 1.01;            // (27 x 32064 x 4096 in int8: 25.6 us as 251 slices on 148 SMs, 23.7 as 126 tiles on 74 pairs)
   if (p.chunks > 65535) cost = 1e300;      // (more than a grid's second dimension holds)
   if (fit && fit->clusters[2] > 0 && T > 16) {
+    // Slices in several rounds start each anew, with nothing under way meanwhile; pairs stay resident and go on reading. 17 to 64 rows,
+    // 22016 to 128256 columns, K 1024 to 8192: as slices int8 2 to 25 % longer, bf16 2 % shorter to 31 % longer; K 64 to 288 with 46 to
+    // 526 rows: 33 to 57 % longer.
+    if (rounds > 1) cost = 1e300;
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
     for (int tn = linear::MAX_TN; tn >= 32; tn -= 32) {
       const int chunks = (T + tn - 1) / tn;

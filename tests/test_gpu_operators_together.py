@@ -403,3 +403,14 @@ def test_context_call_with_another_number_of_rows_leaves_the_drafted_tree(c0, wc
         gpu.close()
     (ma, ea, la), (mb, eb, lb) = results
     assert ma == mb and ea == eb and torch.equal(la, lb)
+
+
+@pytest.mark.parametrize("T,N,K,kind", [(44, 20011, 64, "bf16"), (36, 30020, 24, "f16"), (1674, 4870, 96, "int8"), (17, 40000, 640, "e4m3"),
+                                        (67, 24344, 320, "f16"), (16, 20011, 64, "bf16"), (1, 40000, 48, "int8")])
+def test_linear_of_many_columns_and_few_products(T, N, K, kind):
+    """More tiles of 128 columns than run at once, K of one to five blocks: pairs' many short tiles, slices' rounds up to 16 rows."""
+    g = torch.Generator().manual_seed(T + K)
+    dt = {"bf16": torch.bfloat16, "f16": torch.float16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}[kind]
+    x, w = (torch.randint(-4, 5, s, generator=g) for s in ((T, K), (N, K)))
+    y = _b().linear(x.float().to(dt).cuda(), w.float().to(dt).cuda(), dtype=torch.float32).cpu()
+    assert torch.equal(y.double(), x.double() @ w.double().T)          # whole numbers below 2^24: exact
