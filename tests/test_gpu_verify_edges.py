@@ -88,3 +88,33 @@ def test_rows_that_overlap_are_refused():
     for zc in (z.as_strided((3, 1, 10), (9, 1, 1)), z.as_strided((3, 1, 10), (0, 10, 1)), z.as_strided((3, 1, 10), (10, 10, 2))):
         with pytest.raises(ValueError):
             _b().verify_sampled(zc, i, i, u)
+
+
+@pytest.mark.parametrize("with_probs", [False, True])
+@pytest.mark.parametrize("kind,n,rows,vocab,lo,hi", [
+    (F32, 1, 8, 70000, 0, 70000),               # more pieces than the warps of a cluster keep: a refused child's pass starts from the logits
+    (BF, 2, 12, 70001, 1, 69990),               # the same, rows off every boundary
+    (F32, 1, 6, 1 << 20, 0, 1 << 20),           # as many ids as there may be, all rows at once
+    (BF, 1, 20, (1 << 20) + 3, 2, (1 << 20) + 2),   # row by row
+    (HF, 3, 40, 40000, 5, 39999),               # all rows at once, more than 64 pieces
+    (HF, 3, 100, 40000, 5, 39999),              # row by row
+])
+def test_many_ids(kind, n, rows, vocab, lo, hi, with_probs):
+    """Two children at every other row, several at the root: tokens that are likely, and some that are refused."""
+    g = torch.Generator().manual_seed(vocab + rows)
+    logits = (torch.randn(n, rows, vocab, generator=g) * 4).to(kind)
+    parent = torch.tensor([-1, 0, 0, 0, 0] + [i // 2 * 2 for i in range(3, rows - 2)], dtype=torch.int32)[:rows].repeat(n, 1)
+    probs = torch.softmax((logits.float() + torch.randn(n, rows, vocab, generator=g)), -1) if with_probs else None
+    top = torch.topk(logits[..., lo:hi].float(), 8, dim=-1).indices + lo
+    tokens = torch.zeros(n, rows, dtype=torch.int32)
+    for i in range(1, rows):
+        tokens[:, i] = top[:, int(parent[0, i]), i % 8]
+    met = 0
+    for seed in range(4):
+        u = torch.rand(n, rows, generator=torch.Generator().manual_seed(seed))
+        met += int(check(logits, tokens, parent, u, temperature=(0.1, 1.0, 0.3, 0.2)[seed], draft_probs=probs, lo=lo, hi=hi)[0].sum())
+    u[:, 1:] = 1 - 2.0 ** -24                                        # (nearly) everything is refused
+    for last in (0.0, 0.5, 1 - 2.0 ** -24):
+        u[:, 0] = last
+        check(logits, tokens, parent, u, draft_probs=probs, lo=lo, hi=hi)
+    assert met > 0
