@@ -12,7 +12,7 @@
 // block barrier and no 64-bit arithmetic on its way (the codes that stay open are settled afterwards by their warp alone:
 // with the row's largest value in 64 bits and a second barrier, 4764 rows of 4096 took 69 us, with both but fewer
 // instructions 57), 32 elements a thread (51 with 16) and the next row's copies in flight (47). 4764 x 4096 f32 with a residual
-// to e4m3: 47 us, 5.4 TB/s, bound by HBM; bf16: 26 us. 27 x 4096 bf16: 4.0 us, a launch and three dependent loads. 777 x 4095
+// to e4m3: 46 to 47 us, 5.4 TB/s, bound by HBM; bf16 to int8: 27 us. 27 x 4096 bf16: 4.0 us, a launch and three dependent loads. 777 x 4095
 // f16, whose rows no 16-byte load fits: 10 us, one element per load.
 #pragma once
 #include <cuda_fp16.h>

@@ -15,13 +15,14 @@
 //
 // Two launches, or the second alone (LAZY, below). stats: a warp per (row, 512 ids) leaves their maximum and their sum of exponentials, all rows at once:
 // 22 us for 13.5 M f32 logits (816 rows of 32064 ids, half of them in ragged trees), 20 us for 12.3 M bf16 ones. Its bytes
-// take 8 and 4 us; it issues about 27 instructions a logit, 11 of them 64-bit, and is bound by that. walk: per tree one
+// take 8 and 4 us; it is bound by its instructions, eleven 64-bit ones a logit among them. walk: per tree one
 // CTA, or with draft probabilities a cluster of up to eight that shares the passes over the vocabulary which refused children
 // ask for; rows' sums and the children's weights are gathered in parallel, and without draft probabilities every child is
 // decided at once, so that the walk itself runs from shared memory; the drawn token takes a search over the sums of 512
 // ids and one warp's scan. One tree: 5 to 10 us, nearly all of it latency (dependent loads, 64-bit reductions). Both
 // together: 27 rows x 256 ids 11 us, 51 x 32064 15 us, 64 chains of 6 rows 36 us. Where the trees have many more rows than a walk
-// visits, the cluster sums a row when the walk comes to it: 16 trees of 51 rows with draft probabilities 39 us instead of 46.
+// visits, the cluster sums a row when the walk comes to it: 16 trees of 51 rows with draft probabilities 39 us instead of 46 (39 to 46
+// on other inputs: the longest path counts).
 #pragma once
 #include <cooperative_groups.h>
 #include <algorithm>
@@ -775,7 +776,9 @@ inline cudaError_t enqueue(Args a, const EpArgs &ea, int n_seq, int total_rows, 
   cfg.numAttrs = 1;
   // All rows at once (a microsecond per 1150 pieces), unless they are many more than the walks visit: then row by row as they come
   // to them, which is counted as six rows of every tree at 2.5 us beside their pieces. 16 trees of 51 rows of 32064 ids: 39 us, all at
-  // once 46; 64 chains of 6 rows: 47 and 36. (Paths that go on and on cost their rows.) A context's trees are few and small.
+  // once 46; 64 chains of 6 rows: 47 and 36. What is accepted is not known here, so that deep paths lose: 16 chains of 60 rows, none
+  // accepted 13 us and 47, 52 accepted on average 279 and 53; 64 chains of 64 rows, 4 accepted 35 and 142, 54 accepted 359 and 148;
+  // 4 chains of 128 rows, 66 accepted 477 and 47. A context's trees are few and small.
   const bool lazy = !CTX && (long long)total_rows * a.n_sub > 6 * (2900 + (long long)n_seq * a.n_sub);
   cudaError_t err = cudaSuccess;
   if (!lazy) {
