@@ -390,9 +390,8 @@ int specvla_quantize_rows(const void *X, int type, int rows, int d, long long ld
 
 /* Y = act(X_scale[t] W_scale[n] (X W^T)[t][n] + bias[n]) + residual[t][n]
  * X [T, K] and W [N, K] of one type: BF16, F16, I8 or E4M3; scales only for the last two. int8 sums are exact (32-bit
- * integers, K <= 131071). The others (K <= 2^29) are sums of exact products in the tensor cores' fp32 accumulator, whose additions
- * cut off: off by up to K 2^-23 of the sum of the products' magnitudes, which in fp32 results of long rows is several times
- * the error of a product in fp32 arithmetic. Scales (their product first, which has to be an fp32 number), bias, activation and
+ * integers, K <= 131071). The others (K <= 2^29) are sums of exact products in fp32: for fp32 results as good as fp32 arithmetic
+ * gives them, for 16-bit results with additions that cut off (1.3e-5 of the results' size at K = 11008). Scales (their product first, which has to be an fp32 number), bias, activation and
  * residual are applied in fp32 and the result is rounded once to out_type (F32, BF16, F16). Any T, N, K >= 1; rows of X and W
  * start on 16 bytes (base address and ld); Y and residual on their own element. Y may be the residual itself. Values
  * that are not finite reach what depends on them only.

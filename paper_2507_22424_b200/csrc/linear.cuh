@@ -2,11 +2,8 @@
 //   Y[t][n] = act(sx[t] sw[n] sum_k X[t][k] W[n][k] + bias[n]) + R[t][n]
 // of bf16 or f16 operands, or of int8 codes or e4m3 values with a scale per row of X and of W. int8 sums are exact (32-bit
 // integers); the others are exact products added up in the tensor cores' fp32 accumulator, which cuts off instead of
-// rounding. Everything after them is fp32 and is rounded once, on the way out.
-//
-// What the cut-off costs, against 64 bits (error over the results' size, both root mean square): bf16 rows of 4096 as one
-// accumulator (290 rows) 4.4e-6, where torch's fp32 product has 0.6e-6; of 11008 12e-6 and 1.2e-6; cut into slices of K (27 rows)
-// 1.0e-6 and 2.9e-6. e4m3 codes 0.2e-6 and 0.7e-6. A 16-bit result's own rounding is 1.7e-3 (bf16) or 2e-4 (f16).
+// rounding, and for fp32 results in parts of K (in_parts, below). Everything after them is fp32 and is rounded once, on the
+// way out.
 //
 // The tensor cores take W on their M axis (128 rows a tile) and the rows of X on N, so that a few rows cost a narrow
 // MMA and one pass over W. A K block is 128 bytes of every row (64 or 128 elements): one swizzled row of
@@ -38,6 +35,7 @@ struct Args {
   int T, N, KB;                            // K blocks
   int tn;                                  // rows per chunk = rows of an X box, a multiple of 16
   int act;
+  int part;                                // slices: K blocks per accumulator
   uint32_t idesc;
   int pairs;                               // N is even, and Y and R take two columns at a time
   const float *x_scale, *w_scale, *bias;   // NULL: ones / ones / zeros
@@ -182,6 +180,16 @@ template <int KIND> __device__ __forceinline__ float acc_value(uint32_t r) {
 __host__ __device__ constexpr int stage_bytes(int tn) { return W_BYTES + tn * KBYTES; }
 __host__ __device__ constexpr int stages_of(int tn) { return RING / stage_bytes(tn) < MAX_STAGES ? RING / stage_bytes(tn) : MAX_STAGES; }
 __host__ __device__ constexpr int tmem_cols(int tn) { return tn <= 32 ? 32 : tn <= 64 ? 64 : tn <= 128 ? 128 : 256; }
+// The tensor cores' fp32 additions cut off, which costs a sum 0.15 * 2^-23 of its size per MMA: 4.4e-6 (root mean square, over the
+// results' size) for 290 bf16 rows of 4096 in one accumulator, 12e-6 for 11008, where torch's fp32 product has 0.6e-6 and 1.2e-6. So
+// for fp32 results parts of PART K blocks (32 MMAs) are summed by the tensor cores, and the parts in fp32: 0.5e-6 whatever K
+// (e4m3 codes 0.1e-6). Slices keep a part in each of as many accumulators as tensor memory has; pairs add every part to sums in
+// registers, of at most PART_TN rows, while the next one is under way: 290 x 11008 x 4096 31.4 -> 31.9 us, 4096^3 100 -> 105, 27 x
+// 32064 x 4096 43.7 as before, 1001 x 4332 x 2056 in f16 20.5 -> 29.7 (two rounds of tiles). (PART_TN 160 or 192 spill: 290 rows 36
+// and 45 us. 16-bit results stay as they are: their rounding is 2e-4 (f16) or 1.7e-3 (bf16), the cut-off a sixteenth of it at most.)
+template <int KIND, typename OUT> __host__ __device__ constexpr bool in_parts() { return KIND != KIND_I8 && sizeof(OUT) == 4; }
+constexpr int PART = 8;
+constexpr int PART_TN = 128;
 
 template <typename OUT> struct alignas(2 * sizeof(OUT)) Two { OUT a, b; };
 // One element, or two side by side, into the low bits of r (two floats: r and r1); r keeps its value where p is false. A
@@ -333,7 +341,10 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const int kb0 = (int)((long long)rank * a.KB / S), n_kb = (int)((long long)(rank + 1) * a.KB / S) - kb0;
   const long long row0 = (long long)chunk * a.tn;
   const int T = min(a.T - chunk * a.tn, a.tn);
-  const int cols = tmem_cols(a.tn);
+  constexpr bool PARTS = in_parts<KIND, OUT>();
+  const int width = tmem_cols(a.tn), parts = PARTS ? (n_kb + a.part - 1) / a.part : 1;
+  int cols = width;                                            // a power of two
+  while (PARTS && cols < parts * width) cols *= 2;
   auto fail = [&]() {
     atomicAdd(a.status, 1);
     s_fail = 1;
@@ -386,7 +397,8 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     __syncwarp();
   } else if (warp == 1) {
     const bool lead = elect_one();
-    for (int it = 0, st = 0, ph = 0; it < n_kb; it++) {
+    uint32_t d = tmem;
+    for (int it = 0, st = 0, ph = 0, in = 0; it < n_kb; it++) {
       const bool ok = mbar_wait(full_bar(st), ph, a.wait_ns);
       if (!__all_sync(0xffffffffu, ok)) {
         if (lead) fail();
@@ -396,11 +408,16 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       const uint64_t ad = smem_desc(base + st * stage), bd = smem_desc(base + st * stage + W_BYTES);
       if (lead) {
 #pragma unroll
-        for (int k = 0; k < KBYTES / 32; k++) mma<KIND>(tmem, ad + 2 * k, bd + 2 * k, a.idesc, it > 0 || k > 0);
+        for (int k = 0; k < KBYTES / 32; k++) mma<KIND>(d, ad + 2 * k, bd + 2 * k, a.idesc, in > 0 || k > 0);
         tc_commit(empty_bar(st));
         if (it == n_kb - 1) tc_commit(acc_bar);
       }
       __syncwarp();
+      in++;
+      if (PARTS && in == a.part) {
+        in = 0;
+        d += width;
+      }
       if (++st == stages) {
         st = 0;
         ph ^= 1;
@@ -425,6 +442,15 @@ linear_slice_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       for (int t0 = 0; t0 < T; t0 += 16) {
         uint32_t v[16];
         tc_ld16(ta + t0, v);
+        for (int p = 1; PARTS && p < parts; p++) {
+          uint32_t more[16];
+          tc_ld16(ta + p * width + t0, more);
+          tc_wait_ld();
+          hold(v);
+          hold(more);
+#pragma unroll
+          for (int j = 0; j < 16; j++) v[j] = add_acc<KIND>(v[j], more[j]);
+        }
         if (S == 1) {
           uint32_t r[16] = {};
           residual16<OUT>(a, r, n, t0, T, row0);
@@ -565,8 +591,10 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
+// Says that this warp has read its part of an accumulator. Relaxed: what it orders is tensor memory, which the fences before it and
+// after the wait do; a release would also wait for the warp's stores of results (1000 to 3600 clocks).
 __device__ __forceinline__ void arrive_peer(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 struct PairTiles {
@@ -601,6 +629,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
   const int total = p.tiles * p.chunks;
+  constexpr bool PARTS = in_parts<KIND, OUT>();
   // a wait that gave up: both CTAs of the pair leave in the same way
   auto fail = [&]() {
     atomicAdd(a.status, 1);
@@ -669,7 +698,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       const bool lead = elect_one();
       int st = 0, ph = 0, buf = 0, fph = 1;
       bool ok = true;
-      for (int i = pair; ok && i < total; i += pairs) {
+      const int span = PARTS ? PART : a.KB, per_tile = PARTS ? (a.KB + PART - 1) / PART : 1;
+      // (tiles, or their parts of K, one after the other)
+      for (int i = pair, part = 0; ok && i < total; part + 1 < per_tile ? part++ : (part = 0, i += pairs)) {
         ok = __all_sync(0xffffffffu, mbar_wait(free_bar(buf), fph, a.wait_ns));
         if (!ok) {
           if (lead) fail();
@@ -677,7 +708,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         }
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(buf * MAX_TN);
-        for (int kb = 0; kb < a.KB; kb++) {
+        const int n_kb = PARTS ? min(span, a.KB - part * span) : a.KB;
+        for (int kb = 0; kb < n_kb; kb++) {
           ok = __all_sync(0xffffffffu, mbar_wait(full_bar(st), ph, a.wait_ns));
           if (!ok) {
             if (lead) fail();
@@ -689,7 +721,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
 #pragma unroll
             for (int k = 0; k < KBYTES / 32; k++) mma_pair<KIND>(d, ad + 2 * k, bd + 2 * k, a.idesc, kb > 0 || k > 0);
             commit_pair(empty_bar(st));
-            if (kb == a.KB - 1) commit_pair(acc_bar(buf));
+            if (kb == n_kb - 1) commit_pair(acc_bar(buf));
           }
           __syncwarp();
           if (++st == stages) {
@@ -707,49 +739,99 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   } else {
     const int et = threadIdx.x - 64, q = warp & 3, half = (warp - 2) >> 2, cols = a.tn / 2;
     int buf = 0, ph = 0;
-    for (int i = pair; i < total; i += pairs) {
-      int tile, chunk;
-      tile_at(p, i, tile, chunk);
-      const long long row0 = (long long)chunk * a.tn;
-      const int T = min(a.T - chunk * a.tn, a.tn), n = tile * 2 * BM + (int)rank * BM + q * 32 + lane;
-      const float sw = a.w_scale && n < a.N ? a.w_scale[n] : 1.f, b = a.bias && n < a.N ? a.bias[n] : 0.f;
-      if (a.x_scale && et < a.tn) s_scale[buf][et] = et < T ? a.x_scale[row0 + et] : 1.f;
-      prefetch_residual<OUT>(a, et, 256, tile * 2 * BM + (int)rank * BM, T, row0);
+    // every thread learns whether buffer `buf` holds its sums
+    auto wait_sums = [&]() {
       if (et == 0) {
         const bool ok = mbar_wait(acc_bar(buf), ph, a.wait_ns);
         s_done[buf] = ok;
         if (!ok) fail();
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (!s_done[buf]) break;
-      tc_fence_after();
-      const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN);
-      const int t_end = min((half + 1) * cols, T);
-      uint32_t acc[16], next[16] = {};                          // accumulator and residual, 16 rows ahead
-      residual16<OUT>(a, next, n, half * cols, T, row0);
-      if (half * cols < t_end) tc_ld16(ta + half * cols, acc);
-      for (int t0 = half * cols; t0 < t_end; t0 += 16) {
-        uint32_t r[16];
-        float v[16];
-        tc_wait_ld();
-        hold(acc);
-        scale16<KIND>(a, acc, v, sw, b, s_scale[buf] + t0);
-#pragma unroll
-        for (int k = 0; k < 16; k++) r[k] = next[k];
-        hold(v);
-        hold(r);
-        if (t0 + 16 < t_end) {
-          tc_ld16(ta + t0 + 16, acc);
-          residual16<OUT>(a, next, n, t0 + 16, T, row0);
-        }
-        finish16<OUT>(a, v, r, n, t0, T, row0);
-      }
+      return s_done[buf] != 0;
+    };
+    auto free_sums = [&]() {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive_peer(peer_addr(free_bar(buf), 0));
       if (++buf == 2) {
         buf = 0;
         ph ^= 1;
+      }
+    };
+    for (int i = pair, tile_no = 0; i < total; i += pairs, tile_no++) {
+      int tile, chunk;
+      tile_at(p, i, tile, chunk);
+      const long long row0 = (long long)chunk * a.tn;
+      const int T = min(a.T - chunk * a.tn, a.tn), n = tile * 2 * BM + (int)rank * BM + q * 32 + lane;
+      const float sw = a.w_scale && n < a.N ? a.w_scale[n] : 1.f, b = a.bias && n < a.N ? a.bias[n] : 0.f;
+      const int turn = PARTS ? tile_no & 1 : buf;
+      if (a.x_scale && et < a.tn) s_scale[turn][et] = et < T ? a.x_scale[row0 + et] : 1.f;
+      prefetch_residual<OUT>(a, et, 256, tile * 2 * BM + (int)rank * BM, T, row0);
+      const int t_begin = half * cols, t_end = min((half + 1) * cols, T);
+      if constexpr (PARTS) {
+        constexpr int G = PART_TN / 32;
+        float sum[G][16];
+        bool ok = true;
+        for (int kb = 0; kb < a.KB; kb += PART) {
+          ok = wait_sums();
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN + t_begin);
+#pragma unroll
+          for (int g = 0; g < G; g++) {
+            if (t_begin + 16 * g >= t_end) break;
+            uint32_t acc[16];
+            tc_ld16(ta + 16 * g, acc);
+            tc_wait_ld();
+            hold(acc);
+#pragma unroll
+            for (int j = 0; j < 16; j++) sum[g][j] = kb == 0 ? __uint_as_float(acc[j]) : sum[g][j] + __uint_as_float(acc[j]);
+          }
+          free_sums();
+        }
+        if (!ok) break;
+        uint32_t next[16] = {};
+        residual16<OUT>(a, next, n, t_begin, T, row0);
+#pragma unroll
+        for (int g = 0; g < G; g++) {
+          const int t0 = t_begin + 16 * g;
+          if (t0 >= t_end) break;
+          uint32_t acc[16], r[16];
+          float v[16];
+#pragma unroll
+          for (int k = 0; k < 16; k++) acc[k] = __float_as_uint(sum[g][k]);
+          scale16<KIND>(a, acc, v, sw, b, s_scale[turn] + t0);
+#pragma unroll
+          for (int k = 0; k < 16; k++) r[k] = next[k];
+          hold(v);
+          hold(r);
+          if (t0 + 16 < t_end) residual16<OUT>(a, next, n, t0 + 16, T, row0);
+          finish16<OUT>(a, v, r, n, t0, T, row0);
+        }
+      } else {
+        if (!wait_sums()) break;
+        tc_fence_after();
+        const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * MAX_TN);
+        uint32_t acc[16], next[16] = {};                        // accumulator and residual, 16 rows ahead
+        residual16<OUT>(a, next, n, t_begin, T, row0);
+        if (t_begin < t_end) tc_ld16(ta + t_begin, acc);
+        for (int t0 = t_begin; t0 < t_end; t0 += 16) {
+          uint32_t r[16];
+          float v[16];
+          tc_wait_ld();
+          hold(acc);
+          scale16<KIND>(a, acc, v, sw, b, s_scale[turn] + t0);
+#pragma unroll
+          for (int k = 0; k < 16; k++) r[k] = next[k];
+          hold(v);
+          hold(r);
+          if (t0 + 16 < t_end) {
+            tc_ld16(ta + t0 + 16, acc);
+            residual16<OUT>(a, next, n, t0 + 16, T, row0);
+          }
+          finish16<OUT>(a, v, r, n, t0, T, row0);
+        }
+        free_sums();
       }
     }
     __syncwarp();

@@ -128,8 +128,10 @@ const Fit *cluster_fit() {
 struct Plan {
   bool pair;
   int tn, tiles, chunks, S, grid, raster;
+  int part;                                // slices: K blocks per accumulator
 };
-Plan plan_linear(int T, int N, int KB, const Fit *fit) {
+// parts: fp32 results of parts of K (linear::in_parts).
+Plan plan_linear(int T, int N, int KB, bool parts, const Fit *fit) {
   Plan best = {};
   // few rows: one pass over W, every K block by one CTA; as many slices as run at once, four K blocks each at least
   Plan p = {};
@@ -140,6 +142,8 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   p.S = 1;
   for (int s = 2; fit && s <= linear::MAX_S; s++)
     if ((long long)fit->clusters[s] >= (long long)p.tiles * p.chunks && KB / s >= 4) p.S = s;
+  const int slice = (KB + p.S - 1) / p.S;
+  p.part = std::max(linear::PART, (slice + 512 / linear::tmem_cols(p.tn) - 1) / (512 / linear::tmem_cols(p.tn)));
   best = p;
   // Clocks of a choice: K blocks, whose bytes come from L2 at 64 a clock and SM (slices: 256 + 2 tn, pairs: 256 + tn a block);
   // start, accumulator and exit; slices' hand-over. Neither is done before the weights have been read, at 3440 bytes a clock.
@@ -149,20 +153,22 @@ Plan plan_linear(int T, int N, int KB, const Fit *fit) {
   if (p.S > 1) cost += 2500 + (p.tn / (8 * p.S) + 1) * 1000;
   cost = std::max(cost, read);
   if (p.chunks > 65535) cost = 1e300;      // (more than a grid's second dimension holds)
-  if (fit && fit->clusters[2] > 0 && T > 16) {
+  // (accumulators as tensor memory holds them, of longer parts of K than one and a half times what they should be)
+  const bool coarse = parts && p.part > linear::PART * 3 / 2;
+  if (fit && fit->clusters[2] > 0 && (T > 16 || coarse)) {
     // Slices in several rounds start each anew, with nothing under way meanwhile; pairs stay resident and go on reading. 17 to 64 rows,
     // 22016 to 128256 columns, K 1024 to 8192: as slices int8 2 to 25 % longer, bf16 2 % shorter to 31 % longer; K 64 to 288 with 46 to
     // 526 rows: 33 to 57 % longer.
-    if (rounds > 1) cost = 1e300;
+    if (rounds > 1 || coarse) cost = 1e300;
     const int pairs = fit->clusters[2], tiles = (N + 2 * linear::BM - 1) / (2 * linear::BM);
-    for (int tn = linear::MAX_TN; tn >= 32; tn -= 32) {
+    for (int tn = parts ? linear::PART_TN : linear::MAX_TN; tn >= 32; tn -= 32) {
       const int chunks = (T + tn - 1) / tn;
       if (((T + chunks - 1) / chunks + 31) / 32 * 32 != tn) continue;    // (narrower chunks are no more)
       const long long waves = ((long long)tiles * chunks + pairs - 1) / pairs;
       const double k = std::max(read, waves * (KB * (256. + tn) + 8000 + 24 * tn));
       if (k < cost) {
         cost = k;
-        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2, 0};
+        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2, 0, 0};
       }
     }
   }
@@ -260,9 +266,10 @@ int specvla_linear(const specvla_linear_args *l, void *stream) {
   a.wait_ns = g_linear_wait_ns.exchange(gemm_tc::WAIT_LIMIT_NS);  // the test hook holds for one call
   a.withhold = g_linear_withhold.exchange(0);
   const int kind = l->type == SPECVLA_I8 ? linear::KIND_I8 : l->type == SPECVLA_E4M3 ? linear::KIND_E4M3 : linear::KIND_16;
-  const Plan p = plan_linear(l->T, l->N, a.KB, cluster_fit());
+  const Plan p = plan_linear(l->T, l->N, a.KB, kind != linear::KIND_I8 && l->out_type == SPECVLA_F32, cluster_fit());
   if (!p.pair && p.chunks > 65535) return SPECVLA_ERR_INVALID_ARG;
   a.tn = p.tn;
+  a.part = p.part;
   a.idesc = linear::make_idesc(kind, l->type == SPECVLA_BF16, p.pair ? 2 * linear::BM : linear::BM, a.tn);
   CUtensorMap mw, mx;
   if (!linear::make_map(&mw, l->W, l->N, bytes, ldw, linear::BM) || !linear::make_map(&mx, l->X, l->T, bytes, ldx, p.pair ? a.tn / 2 : a.tn)) {
