@@ -35,7 +35,7 @@ struct Args {
   int T, N, KB;                            // K blocks
   int tn;                                  // rows per chunk = rows of an X box, a multiple of 16
   int act;
-  int part;                                // slices: K blocks per accumulator
+  int part;                                // K blocks per accumulator (in_parts)
   uint32_t idesc;
   int pairs;                               // N is even, and Y and R take two columns at a time
   const float *x_scale, *w_scale, *bias;   // NULL: ones / ones / zeros
@@ -182,13 +182,14 @@ __host__ __device__ constexpr int stages_of(int tn) { return RING / stage_bytes(
 __host__ __device__ constexpr int tmem_cols(int tn) { return tn <= 32 ? 32 : tn <= 64 ? 64 : tn <= 128 ? 128 : 256; }
 // The tensor cores' fp32 additions cut off, which costs a sum 0.15 * 2^-23 of its size per MMA: 4.4e-6 (root mean square, over the
 // results' size) for 290 bf16 rows of 4096 in one accumulator, 12e-6 for 11008, where torch's fp32 product has 0.6e-6 and 1.2e-6. So
-// for fp32 results parts of PART K blocks (32 MMAs) are summed by the tensor cores, and the parts in fp32: 0.5e-6 whatever K
-// (e4m3 codes 0.1e-6). Slices keep a part in each of as many accumulators as tensor memory has; pairs add every part to sums in
-// registers, of at most PART_TN rows, while the next one is under way: 290 x 11008 x 4096 31.4 -> 31.9 us, 4096^3 100 -> 105, 27 x
-// 32064 x 4096 43.7 as before, 1001 x 4332 x 2056 in f16 20.5 -> 29.7 (two rounds of tiles). (PART_TN 160 or 192 spill: 290 rows 36
-// and 45 us. 16-bit results stay as they are: their rounding is 2e-4 (f16) or 1.7e-3 (bf16), the cut-off a sixteenth of it at most.)
+// for fp32 results parts of K are summed by the tensor cores, and the parts in fp32: a quarter of K each, at most 4 K blocks (16
+// MMAs) in slices and 8 in pairs, 0.24e-6 and 0.47e-6 whatever K. Slices keep a part in each of as many accumulators as tensor
+// memory has; pairs add every part to sums in registers, of at most PART_TN rows, while the next one is under way: 290 x 11008 x
+// 4096 31.4 -> 32.2 us (parts of 4 33.9), 4096^3 100 -> 105 (115), 27 x 32064 x 4096 43.7 as before, 1001 x 4332 x 2056 in f16 22 -> 29
+// (two rounds of tiles). (PART_TN 160 or 192 spill: 290 rows 36 and 45 us. 16-bit results stay as they are: their rounding
+// is 2e-4 (f16) or 1.7e-3 (bf16), the cut-off a sixteenth of it at most.)
 template <int KIND, typename OUT> __host__ __device__ constexpr bool in_parts() { return KIND != KIND_I8 && sizeof(OUT) == 4; }
-constexpr int PART = 8;
+constexpr int SLICE_PART = 4, PAIR_PART = 8;
 constexpr int PART_TN = 128;
 
 template <typename OUT> struct alignas(2 * sizeof(OUT)) Two { OUT a, b; };
@@ -698,7 +699,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       const bool lead = elect_one();
       int st = 0, ph = 0, buf = 0, fph = 1;
       bool ok = true;
-      const int span = PARTS ? PART : a.KB, per_tile = PARTS ? (a.KB + PART - 1) / PART : 1;
+      const int per_tile = PARTS ? (a.KB + a.part - 1) / a.part : 1;
       // (tiles, or their parts of K, one after the other)
       for (int i = pair, part = 0; ok && i < total; part + 1 < per_tile ? part++ : (part = 0, i += pairs)) {
         ok = __all_sync(0xffffffffu, mbar_wait(free_bar(buf), fph, a.wait_ns));
@@ -708,7 +709,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         }
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(buf * MAX_TN);
-        const int n_kb = PARTS ? min(span, a.KB - part * span) : a.KB;
+        const int n_kb = PARTS ? min(a.part, a.KB - part * a.part) : a.KB;
         for (int kb = 0; kb < n_kb; kb++) {
           ok = __all_sync(0xffffffffu, mbar_wait(full_bar(st), ph, a.wait_ns));
           if (!ok) {
@@ -772,7 +773,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         constexpr int G = PART_TN / 32;
         float sum[G][16];
         bool ok = true;
-        for (int kb = 0; kb < a.KB; kb += PART) {
+        for (int kb = 0; kb < a.KB; kb += a.part) {
           ok = wait_sums();
           if (!ok) break;
           tc_fence_after();

@@ -128,7 +128,7 @@ const Fit *cluster_fit() {
 struct Plan {
   bool pair;
   int tn, tiles, chunks, S, grid, raster;
-  int part;                                // slices: K blocks per accumulator
+  int part;                                // K blocks per accumulator (linear::in_parts)
 };
 // parts: fp32 results of parts of K (linear::in_parts).
 Plan plan_linear(int T, int N, int KB, bool parts, const Fit *fit) {
@@ -142,8 +142,8 @@ Plan plan_linear(int T, int N, int KB, bool parts, const Fit *fit) {
   p.S = 1;
   for (int s = 2; fit && s <= linear::MAX_S; s++)
     if ((long long)fit->clusters[s] >= (long long)p.tiles * p.chunks && KB / s >= 4) p.S = s;
-  const int slice = (KB + p.S - 1) / p.S;
-  p.part = std::max(linear::PART, (slice + 512 / linear::tmem_cols(p.tn) - 1) / (512 / linear::tmem_cols(p.tn)));
+  const int slice = (KB + p.S - 1) / p.S, held = 512 / linear::tmem_cols(p.tn), quarter = std::max(1, KB / 4);
+  p.part = std::max(std::min(quarter, linear::SLICE_PART), (slice + held - 1) / held);
   best = p;
   // Clocks of a choice: K blocks, whose bytes come from L2 at 64 a clock and SM (slices: 256 + 2 tn, pairs: 256 + tn a block);
   // start, accumulator and exit; slices' hand-over. Neither is done before the weights have been read, at 3440 bytes a clock.
@@ -153,8 +153,8 @@ Plan plan_linear(int T, int N, int KB, bool parts, const Fit *fit) {
   if (p.S > 1) cost += 2500 + (p.tn / (8 * p.S) + 1) * 1000;
   cost = std::max(cost, read);
   if (p.chunks > 65535) cost = 1e300;      // (more than a grid's second dimension holds)
-  // (accumulators as tensor memory holds them, of longer parts of K than one and a half times what they should be)
-  const bool coarse = parts && p.part > linear::PART * 3 / 2;
+  // (tensor memory holds too few accumulators for parts of K about as short as a pair's)
+  const bool coarse = parts && p.part > linear::PAIR_PART * 3 / 2;
   if (fit && fit->clusters[2] > 0 && (T > 16 || coarse)) {
     // Slices in several rounds start each anew, with nothing under way meanwhile; pairs stay resident and go on reading. 17 to 64 rows,
     // 22016 to 128256 columns, K 1024 to 8192: as slices int8 2 to 25 % longer, bf16 2 % shorter to 31 % longer; K 64 to 288 with 46 to
@@ -168,7 +168,7 @@ Plan plan_linear(int T, int N, int KB, bool parts, const Fit *fit) {
       const double k = std::max(read, waves * (KB * (256. + tn) + 8000 + 24 * tn));
       if (k < cost) {
         cost = k;
-        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2, 0, 0};
+        best = {true, tn, tiles, chunks, 1, (int)std::min<long long>(pairs, (long long)tiles * chunks) * 2, 0, std::min(quarter, linear::PAIR_PART)};
       }
     }
   }

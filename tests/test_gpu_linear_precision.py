@@ -27,3 +27,19 @@ def test_fp32_results(T, N, K, kind):
     assert off <= 12 * 2.0 ** -23, float(off) * 2 ** 23
     assert torch.equal(B.linear(x, w, dtype=F32).double(), y)
     B.linear_status()
+
+
+@pytest.mark.parametrize("kind", [BF, HF])
+@pytest.mark.parametrize("K", [64, 200, 256, 512, 1024, 2048])
+@pytest.mark.parametrize("T,N", [(5, 2000), (300, 2000)])
+def test_fp32_results_of_short_rows(T, N, K, kind):
+    """A quarter of a row in each accumulator, one K block (4 MMAs of 16) at least and 8 at most: at 0.24 * 2^-23 per MMA of a part, as
+    above, and half a unit at most (2^-24) for each of the up to four additions of parts and for the result, over its size."""
+    from paper_2507_22424_b200 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T + K)
+    x = torch.randn(T, K, generator=g, device="cuda").to(kind)
+    w = torch.randn(N, K, generator=g, device="cuda").to(kind)
+    y, want = B.linear(x, w, dtype=F32).double(), x.double() @ w.double().T
+    off = ((y - want).pow(2).mean() / want.pow(2).mean()).sqrt()
+    mmas = 4 * min(8, max(1, (K + 63) // 64 // 4))
+    assert off <= (0.24 * mmas + 2.5) * 2.0 ** -23, float(off) * 2 ** 23
