@@ -24,12 +24,9 @@ def check(logits, tokens, parent, u, **kw):
     return want
 
 
-@pytest.mark.parametrize("rows", [4, 60])
-@pytest.mark.parametrize("vocab", [40, 700])
-def test_little_is_left_after_refused_tokens(rows, vocab):
+def check_little_left(n, rows, vocab):
     """Two siblings with nearly all of the weight are refused; the third is decided by a random number 2^-20 beside its share of
-    what is left (1e-14 of the row): what is left has to be right relative to itself. rows = 60: summed as the walk comes to them."""
-    n = 400 if rows == 60 else 64
+    what is left (1e-14 of the row): what is left has to be right relative to itself."""
     g = torch.Generator().manual_seed(vocab)
     logits = torch.full((n, rows, vocab), -60.0)
     logits[:, 0, 3] = 0.0
@@ -52,6 +49,17 @@ def test_little_is_left_after_refused_tokens(rows, vocab):
     # (a first token with more than 1 - 2^-24 of the weight is accepted)
     third = (w[:, 3] / w.sum(1) <= u[:, 1].double()) & (w[:, vocab - 2] / (w.sum(1) - w[:, 3]) <= u[:, 2].double())
     assert torch.equal(m[third], (~up).int()[third]) and third.sum() > n // 4
+
+
+@pytest.mark.parametrize("n,rows", [(64, 4), (400, 60)])            # all rows at once; as the walk comes to them
+@pytest.mark.parametrize("vocab", [40, 700])
+def test_little_is_left_after_refused_tokens(n, rows, vocab):
+    check_little_left(n, rows, vocab)
+
+
+def test_little_is_left_where_a_cluster_shares_a_row():
+    """Row by row over the whole vocabulary: every CTA of a cluster comes to the same decision."""
+    check_little_left(8, 64, 32064)
 
 
 @pytest.mark.parametrize("with_probs", [False, True])
